@@ -510,6 +510,180 @@ int lynx_hkv_dequant(const lynx_layout *L, int32_t b, int32_t T, const int32_t *
                      int32_t variant, const lynx_hmeta *meta, void *k_out_bf16, void *v_out_bf16,
                      void *stream);
 
+/*
+ * Trees of drafted tokens.  A speculative decoder that is unsure of a token
+ * drafts several in its place, and the drafts of a step form a tree: parents
+ * (int32 [B][n], 1 <= n <= 64 nodes) holds for node i the number of the node
+ * it follows, -1 for a node that follows the context.  A node comes after its
+ * parent: a value outside -1 .. i - 1 marks node i as not there (the padding
+ * of a shorter tree), and nothing below such a node is there either.  A chain
+ * (parents 0 .. n - 1 less one) is the linear case of lynx_attn_verify and
+ * lynx_spec_accept_greedy.
+ */
+
+/*
+ * lynx_attn_verify_tree -- the verification pass (Sec. 4.3) over a tree: node
+ * i's query attends the whole context (the merged 8-bit cache, zero + code *
+ * scale) and, of the nodes, its ancestors and itself, by their own BF16 K/V.
+ *
+ *   n            nodes per sequence, 1 <= n <= 64; B <= 65535
+ *   q_bf16       BF16 [B][n][Hq][128] (device)
+ *   k_new, v_new BF16 [B][n][Hkv][128] (device)
+ *   parents      int32 [B][n] (device), as above
+ *   out_bf16     BF16 [B][n][Hq][128] (device, written); rows of nodes that
+ *                are not there are 0
+ *   other arguments as lynx_attn_verify; workspace >=
+ *   lynx_attn_workspace_bytes(L, B, Hq, n, max_seq_len)
+ * A node's K and V reach the rows of its descendants and its own alone,
+ * whatever they hold (NaN and infinities included).
+ */
+int lynx_attn_verify_tree(const lynx_layout *L, int32_t B, int32_t Hq, int32_t n,
+                          int32_t max_seq_len, const int32_t *seq_lens, const int32_t *block_table,
+                          const uint8_t *k_codes, const uint8_t *v_codes, const lynx_meta *meta,
+                          const void *q_bf16, const void *k_new, const void *v_new,
+                          const int32_t *parents, void *out_bf16, void *workspace,
+                          size_t workspace_bytes, void *stream);
+
+/*
+ * lynx_spec_tree_workspace_bytes -- device workspace of the two acceptance
+ * calls below for B sequences (<= 65535), n nodes and a vocabulary of `vocab`
+ * entries (1..2^23).  Returns 0 on invalid arguments.  Zero the workspace
+ * once, before its first use; every call leaves it zero, so calls of any
+ * shape can share one that is large enough.  Calls that share a workspace
+ * must not run concurrently.
+ */
+size_t lynx_spec_tree_workspace_bytes(int32_t B, int32_t n, int32_t vocab);
+
+/*
+ * lynx_spec_accept_tree_greedy -- greedy acceptance over a tree (Sec. 4.3:
+ * keep what the target model agrees with, correct the first divergence).  A
+ * row's choice is its highest score, the lowest vocabulary index among equal
+ * ones (a NaN never wins; a row of NaNs alone has the choice -1).  From the
+ * context on, the walk goes to the child whose token is the current row's
+ * choice, the lowest such node where several hold it, and ends where there is
+ * none.  A node whose token is outside [0, vocab) is never kept.
+ *
+ *   target_logits  fp32 [B][n+1][vocab] (device): row 0 the target's scores
+ *                  for the token after the context, row j + 1 for the token
+ *                  after node j; rows off the path may hold anything
+ *   tokens         int32 [B][n] (device): the nodes' tokens
+ *   parents        int32 [B][n] (device), as above
+ *   accepted       int32 [B] (device, written): nodes kept (0..n)
+ *   path           int32 [B][n] (device, written): their numbers in order
+ *                  from the context on, then -1
+ *   next_token     int32 [B] (device, written): the choice after the last
+ *                  node kept
+ *   workspace      >= lynx_spec_tree_workspace_bytes(B, n, vocab)
+ *                  (LYNX_EWORKSPACE otherwise), zero as described there
+ */
+int lynx_spec_accept_tree_greedy(int32_t B, int32_t n, int32_t vocab, const float *target_logits,
+                                 const int32_t *tokens, const int32_t *parents, int32_t *accepted,
+                                 int32_t *path, int32_t *next_token, void *workspace,
+                                 size_t workspace_bytes, void *stream);
+
+/*
+ * lynx_spec_accept_tree_sample -- the same with drawn choices: a row's choice
+ * is a draw from its probabilities with the row's own uniform, by the exact
+ * rule of lynx_spec_accept_sample (weights floor(p 2^40), so the outcome
+ * depends on the inputs alone; a row of zero weights has the choice -1).
+ * Every emitted token is a draw from the target's row at its place, so the
+ * emitted tokens are distributed as the target model's, whatever the tree; a
+ * node is kept with the target's probability of its token.
+ *
+ *   target_probs   fp32 [B][n+1][vocab] (device)
+ *   uniforms       fp32 [B][n+1] (device): uniform numbers in [0, 1), one a row
+ *   other arguments as lynx_spec_accept_tree_greedy
+ */
+int lynx_spec_accept_tree_sample(int32_t B, int32_t n, int32_t vocab, const float *target_probs,
+                                 const int32_t *tokens, const int32_t *parents,
+                                 const float *uniforms, int32_t *accepted, int32_t *path,
+                                 int32_t *next_token, void *workspace, size_t workspace_bytes,
+                                 void *stream);
+
+/*
+ * The cache written token by token.  A K group's scale is known only when its
+ * 128 tokens are there, so the BF16 K rows of the last group begun (the open
+ * one) are kept beside the cache, and an append quantizes the open group
+ * again: planes and metadata are at all times those of lynx_kv_encode over
+ * the whole sequence (merged by lynx_kv_merge), bit for bit.
+ *   k_open  BF16 [B][LYNX_OPEN_ROWS][Hkv][128]: row t % LYNX_OPEN_ROWS holds
+ *           the K of token t, for the tokens of the open group and of the
+ *           group before it.  It needs no initialisation for an empty
+ *           sequence.  One per layer, as the planes and the metadata are.
+ * The group before the open one lets a length be taken back (drafts undone): to
+ * any length from the start of the group before the open one of the longest
+ * length so far.  The next append quantizes the open group from its rows again,
+ * to the same bits; until then it keeps codes and scales that the tokens taken
+ * back had a part in.
+ */
+#define LYNX_OPEN_ROWS 256
+
+/*
+ * lynx_kv_append -- quantize tokens into the cache behind the ones it holds.
+ *
+ *   B            sequences (<= 65535)
+ *   max_new      tokens per sequence at most (<= 8000000)
+ *   n_src        rows of k_new and v_new per sequence
+ *   seq_lens     int32 [B] (device): lengths before the append.  They are not
+ *                changed: the caller adds the counts once every layer has been
+ *                appended to
+ *   counts       int32 [B] (device): tokens to append, clamped to 0..max_new
+ *                (`accepted` of a tree's acceptance); tokens that
+ *                min(max_tokens, max_blocks_per_seq * bt) leaves no room for
+ *                are not appended
+ *   path         int32 [B][max_new] (device): the row of k_new and v_new that
+ *                holds new token i (`path` of a tree's acceptance; the same
+ *                row may stand twice); the tokens from the first entry outside
+ *                [0, n_src) on are not appended.  max_new <= 64 then.  Or
+ *                NULL: row i, and n_src >= max_new
+ *   k_new, v_new BF16 [B][n_src][Hkv][128] (device, read)
+ *   k_open       as above (device, read and written)
+ *   k_codes, v_codes   code planes of 128-byte rows
+ *   k_anc, v_anc, k_res, v_res   nibble planes
+ *                (device, written: the new tokens, and of K the whole open
+ *                group); each pair may be NULL, one must be given
+ *   meta         metadata of the batch (device, written for the same tokens)
+ * Rows whose block id is outside [0, num_blocks) are skipped.  Blocks that
+ * hold tokens of an open group must not be shared between sequences.
+ */
+int lynx_kv_append(const lynx_layout *L, int32_t B, int32_t max_new, int32_t n_src,
+                   const int32_t *seq_lens, const int32_t *counts, const int32_t *path,
+                   const int32_t *block_table, const void *k_new, const void *v_new, void *k_open,
+                   uint8_t *k_codes, uint8_t *v_codes, uint8_t *k_anc, uint8_t *v_anc,
+                   uint8_t *k_res, uint8_t *v_res, const lynx_meta *meta, void *stream);
+
+/*
+ * lynx_kv_append_begin -- fill k_open for sequences whose BF16 K is not at
+ * hand (their context was transferred): the open group and the one before it
+ * are read back from the merged codes (as lynx_kv_dequant).  Appends then
+ * quantize the open group from these values.
+ *   seq_lens     int32 [B] (device): lengths; tokens past
+ *                min(max_tokens, max_blocks_per_seq * bt) are ignored
+ *   k_open       BF16 [B][LYNX_OPEN_ROWS][Hkv][128] (device, written)
+ */
+int lynx_kv_append_begin(const lynx_layout *L, int32_t B, const int32_t *seq_lens,
+                         const int32_t *block_table, const uint8_t *k_codes, const lynx_meta *meta,
+                         void *k_open, void *stream);
+
+/*
+ * lynx_kv_dequant -- read the merged cache back: tokens starts[b] ..
+ * starts[b] + counts[b] - 1 of every sequence as BF16, x = fmaf(code, scale,
+ * zero) in fp32, rounded to nearest even.
+ *   max_n        rows of the outputs per sequence (<= 8000000)
+ *   starts       int32 [B] (device); a negative start, or one at or past
+ *                min(max_tokens, max_blocks_per_seq * bt), reads nothing
+ *   counts       int32 [B] (device), clamped to 0..max_n and to that bound
+ *   k_codes, v_codes  code planes (device)
+ *   k_out_bf16, v_out_bf16  BF16 [B][max_n][Hkv][128] (device, written): row i
+ *                holds token starts[b] + i; rows from counts[b] on, and rows
+ *                whose block id is outside [0, num_blocks), are left as they
+ *                were
+ */
+int lynx_kv_dequant(const lynx_layout *L, int32_t B, int32_t max_n, const int32_t *starts,
+                    const int32_t *counts, const int32_t *block_table, const uint8_t *k_codes,
+                    const uint8_t *v_codes, const lynx_meta *meta, void *k_out_bf16,
+                    void *v_out_bf16, void *stream);
+
 /* Static, human-readable text for a lynx_status value. */
 const char *lynx_strerror(int status);
 

@@ -540,3 +540,188 @@ int lynx_hkv_dequant(const lynx_layout *L, int32_t b, int32_t T, const int32_t *
 }
 
 }  // extern "C"
+
+namespace {
+int bt_shift_of(int bt) {
+    for (int sh = 0; sh < 31; ++sh)
+        if ((1 << sh) == bt) return sh;
+    return -1;
+}
+// Sequences, and 128-token groups per sequence, that a launch's grid holds.
+constexpr int kMostB = 65535;
+constexpr int kMostTokens = 8000000;  // 62502 groups
+static_assert(LYNX_OPEN_ROWS == lynx::kOpenRows, "header and library disagree");
+}  // namespace
+
+extern "C" {
+
+int lynx_attn_verify_tree(const lynx_layout *L, int32_t B, int32_t Hq, int32_t n, int32_t max_seq_len,
+                          const int32_t *seq_lens, const int32_t *block_table, const uint8_t *k_codes,
+                          const uint8_t *v_codes, const lynx_meta *meta, const void *q_bf16, const void *k_new,
+                          const void *v_new, const int32_t *parents, void *out_bf16, void *workspace,
+                          size_t workspace_bytes, void *stream) {
+    Geometry g;
+    MetaPtrs mp;
+    int rc = check_attention_common(L, B, Hq, max_seq_len, seq_lens, block_table, k_codes, v_codes, meta, q_bf16,
+                                    out_bf16, &g, &mp);
+    if (rc != LYNX_OK) return rc;
+    if (n < 1 || n > 64 || B > kMostB) return LYNX_EINVAL;
+    if (B == 0) return LYNX_OK;
+    const void *ptrs[] = {k_new, v_new, parents};
+    for (const void *p : ptrs)
+        if (!p || !aligned16(p)) return LYNX_EINVAL;
+    const lynx::AttnPlan p = lynx::plan_attention(lynx::KvMode::kCodes, g, B, Hq, n, max_seq_len);
+    if (!workspace || !aligned16(workspace) ||
+        workspace_bytes < lynx::attention_workspace_bound(g, B, Hq, n, max_seq_len))
+        return LYNX_EWORKSPACE;
+    hipError_t e = lynx::launch_verify_tree(
+        g, p, B, Hq, n, max_seq_len, seq_lens, block_table, k_codes, v_codes, mp, static_cast<const uint16_t *>(q_bf16),
+        static_cast<const uint16_t *>(k_new), static_cast<const uint16_t *>(v_new), parents,
+        static_cast<uint16_t *>(out_bf16), workspace, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? LYNX_OK : LYNX_EHIP;
+}
+
+size_t lynx_spec_tree_workspace_bytes(int32_t B, int32_t n, int32_t vocab) {
+    if (B < 0 || B > kMostB || n < 1 || n > 64 || vocab < 1 || vocab > (1 << 23)) return 0;
+    return lynx::spec_tree_workspace(B, n, vocab);
+}
+
+}  // extern "C"
+
+namespace {
+int accept_tree(int32_t B, int32_t n, int32_t vocab, const float *scores, const int32_t *tokens,
+                const int32_t *parents, const float *uniforms, int32_t *accepted, int32_t *path,
+                int32_t *next_token, void *workspace, size_t workspace_bytes, void *stream) {
+    if (B < 0 || B > kMostB || n < 1 || n > 64 || vocab < 1 || vocab > (1 << 23)) return LYNX_EINVAL;
+    if (B == 0) return LYNX_OK;
+    const void *ptrs[] = {scores, tokens, parents, accepted, path, next_token};
+    for (const void *p : ptrs)
+        if (!p || !aligned16(p)) return LYNX_EINVAL;
+    if (!workspace || !aligned16(workspace) || workspace_bytes < lynx_spec_tree_workspace_bytes(B, n, vocab))
+        return LYNX_EWORKSPACE;
+    lynx::TreeAcceptArgs a{};
+    a.n = n;
+    a.vocab = vocab;
+    a.scores = scores;
+    a.tokens = tokens;
+    a.parents = parents;
+    a.uniforms = uniforms;
+    a.accepted = accepted;
+    a.path = path;
+    a.next_token = next_token;
+    hipError_t e = lynx::launch_spec_accept_tree(a, B, workspace, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? LYNX_OK : LYNX_EHIP;
+}
+}  // namespace
+
+extern "C" {
+
+int lynx_spec_accept_tree_greedy(int32_t B, int32_t n, int32_t vocab, const float *target_logits,
+                                 const int32_t *tokens, const int32_t *parents, int32_t *accepted, int32_t *path,
+                                 int32_t *next_token, void *workspace, size_t workspace_bytes, void *stream) {
+    return accept_tree(B, n, vocab, target_logits, tokens, parents, nullptr, accepted, path, next_token, workspace,
+                       workspace_bytes, stream);
+}
+
+int lynx_spec_accept_tree_sample(int32_t B, int32_t n, int32_t vocab, const float *target_probs,
+                                 const int32_t *tokens, const int32_t *parents, const float *uniforms,
+                                 int32_t *accepted, int32_t *path, int32_t *next_token, void *workspace,
+                                 size_t workspace_bytes, void *stream) {
+    if (B > 0 && (!uniforms || !aligned16(uniforms))) return LYNX_EINVAL;
+    return accept_tree(B, n, vocab, target_probs, tokens, parents, uniforms, accepted, path, next_token, workspace,
+                       workspace_bytes, stream);
+}
+
+int lynx_kv_append(const lynx_layout *L, int32_t B, int32_t max_new, int32_t n_src, const int32_t *seq_lens,
+                   const int32_t *counts, const int32_t *path, const int32_t *block_table, const void *k_new,
+                   const void *v_new, void *k_open, uint8_t *k_codes, uint8_t *v_codes, uint8_t *k_anc,
+                   uint8_t *v_anc, uint8_t *k_res, uint8_t *v_res, const lynx_meta *meta, void *stream) {
+    Geometry g;
+    MetaPtrs mp;
+    int rc = check_layout(L, &g);
+    if (rc != LYNX_OK) return rc;
+    if ((rc = check_meta(meta, &mp)) != LYNX_OK) return rc;
+    if (B < 0 || B > kMostB || max_new < 0 || max_new > kMostTokens || n_src < 0) return LYNX_EINVAL;
+    if (path ? max_new > 64 : n_src < max_new) return LYNX_EINVAL;
+    if ((k_codes == nullptr) != (v_codes == nullptr) || (k_anc == nullptr) != (v_anc == nullptr) ||
+        (k_res == nullptr) != (v_res == nullptr) || (!k_codes && !k_anc && !k_res))
+        return LYNX_EINVAL;
+    if (B == 0 || max_new == 0) return LYNX_OK;
+    const void *ptrs[] = {seq_lens, counts, block_table, k_new, v_new, k_open};
+    for (const void *p : ptrs)
+        if (!p || !aligned16(p)) return LYNX_EINVAL;
+    const void *may_be_null[] = {path, k_codes, v_codes, k_anc, v_anc, k_res, v_res};
+    for (const void *p : may_be_null)
+        if (!aligned16(p)) return LYNX_EINVAL;
+    lynx::AppendArgs a;
+    a.geo = g;
+    a.max_new = max_new;
+    a.n_src = n_src;
+    a.capacity = (int)layout_capacity(g);
+    a.bt_shift = bt_shift_of(g.bt);
+    a.seq_lens = seq_lens;
+    a.counts = counts;
+    a.path = path;
+    a.block_table = block_table;
+    a.k_new = static_cast<const uint16_t *>(k_new);
+    a.v_new = static_cast<const uint16_t *>(v_new);
+    a.k_open = static_cast<uint16_t *>(k_open);
+    a.codes[0] = k_codes;
+    a.codes[1] = v_codes;
+    a.anc[0] = k_anc;
+    a.anc[1] = v_anc;
+    a.res[0] = k_res;
+    a.res[1] = v_res;
+    a.meta = mp;
+    hipError_t e = lynx::launch_append(a, B, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? LYNX_OK : LYNX_EHIP;
+}
+
+int lynx_kv_append_begin(const lynx_layout *L, int32_t B, const int32_t *seq_lens, const int32_t *block_table,
+                         const uint8_t *k_codes, const lynx_meta *meta, void *k_open, void *stream) {
+    lynx::DequantArgs a{};
+    int rc = check_layout(L, &a.geo);
+    if (rc != LYNX_OK) return rc;
+    if ((rc = check_meta(meta, &a.meta)) != LYNX_OK) return rc;
+    if (B < 0 || B > kMostB) return LYNX_EINVAL;
+    if (B == 0) return LYNX_OK;
+    const void *ptrs[] = {seq_lens, block_table, k_codes, k_open};
+    for (const void *p : ptrs)
+        if (!p || !aligned16(p)) return LYNX_EINVAL;
+    a.capacity = (int)layout_capacity(a.geo);
+    a.bt_shift = bt_shift_of(a.geo.bt);
+    a.starts = seq_lens;
+    a.block_table = block_table;
+    a.k_codes = k_codes;
+    a.k_out = static_cast<uint16_t *>(k_open);
+    hipError_t e = lynx::launch_append_begin(a, B, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? LYNX_OK : LYNX_EHIP;
+}
+
+int lynx_kv_dequant(const lynx_layout *L, int32_t B, int32_t max_n, const int32_t *starts, const int32_t *counts,
+                    const int32_t *block_table, const uint8_t *k_codes, const uint8_t *v_codes,
+                    const lynx_meta *meta, void *k_out_bf16, void *v_out_bf16, void *stream) {
+    lynx::DequantArgs a{};
+    int rc = check_layout(L, &a.geo);
+    if (rc != LYNX_OK) return rc;
+    if ((rc = check_meta(meta, &a.meta)) != LYNX_OK) return rc;
+    if (B < 0 || B > kMostB || max_n < 0 || max_n > kMostTokens) return LYNX_EINVAL;
+    if (B == 0 || max_n == 0) return LYNX_OK;
+    const void *ptrs[] = {starts, counts, block_table, k_codes, v_codes, k_out_bf16, v_out_bf16};
+    for (const void *p : ptrs)
+        if (!p || !aligned16(p)) return LYNX_EINVAL;
+    a.max_n = max_n;
+    a.capacity = (int)layout_capacity(a.geo);
+    a.bt_shift = bt_shift_of(a.geo.bt);
+    a.starts = starts;
+    a.counts = counts;
+    a.block_table = block_table;
+    a.k_codes = k_codes;
+    a.v_codes = v_codes;
+    a.k_out = static_cast<uint16_t *>(k_out_bf16);
+    a.v_out = static_cast<uint16_t *>(v_out_bf16);
+    hipError_t e = lynx::launch_dequant(a, B, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? LYNX_OK : LYNX_EHIP;
+}
+
+}  // extern "C"

@@ -1,0 +1,276 @@
+// The cache written as tokens are kept, and read back (gfx950).
+//
+// A K group is 128 consecutive tokens of one channel, so its scale is known
+// only when the group is whole.  Until then the group is open: its rows stay
+// in BF16 too, in a ring of 256 rows per sequence (row t % 256 holds token t),
+// and every append quantizes the whole open group again from them.  The cache
+// is therefore at all times what lynx_kv_encode of the whole sequence gives,
+// bit for bit, and the attention kernels need no case for an open group.  V
+// groups are single tokens: only the new ones are quantized.
+//
+// What bounds it: a decode step's append moves at most 128 K rows of a head,
+// so it is a chain of dependent loads (length, rows, group extrema, stores); a
+// chunk of a prompt reads 4 bytes and writes 2 per element pair and is bound
+// by memory.
+#include "lane_ops.h"
+#include "lynx_internal.h"
+#include "quantize.h"
+
+namespace lynx {
+namespace {
+
+constexpr int kThreads = 256;
+constexpr int kRing = kOpenRows;
+
+// Row index of (kv head h, token t) of a sequence in a plane pool, or -1 where
+// the block table names no valid block.
+__device__ __forceinline__ long long pool_row(const Geometry &g, const int32_t *bt_row, int bt_shift, int h, int t) {
+    const int bi = bt_shift >= 0 ? (t >> bt_shift) : t / g.bt;
+    const int blk = bt_row[bi];
+    if (blk < 0 || blk >= g.num_blocks) return -1;
+    return ((long long)blk * g.Hkv + h) * g.bt + (t - bi * g.bt);
+}
+
+// Codes of 8 dims (8 m .. + 7) into every plane that the caller gave.
+__device__ __forceinline__ void store_codes(const AppendArgs &a, int which, const float *x, const float *zero,
+                                            const float *inv, long long row, int m) {
+    const uint64_t c = quantize8(x, zero, inv);
+    if (a.codes[which]) *reinterpret_cast<uint64_t *>(a.codes[which] + row * kCodeRow + 8 * m) = c;
+    if (a.anc[which] || a.res[which]) {
+        uint32_t an, rs;
+        quantize_split8(x, zero, inv, an, rs);
+        if (a.anc[which]) *reinterpret_cast<uint32_t *>(a.anc[which] + row * kNibbleRow + 4 * m) = an;
+        if (a.res[which]) *reinterpret_cast<uint32_t *>(a.res[which] + row * kNibbleRow + 4 * m) = rs;
+    }
+}
+
+// Tokens appended to sequence b: the count, less what the cache has no room for
+// and what follows the first entry of the path that names no row.
+__device__ __forceinline__ int appended(const AppendArgs &a, int b, int T) {
+    int n = min(max(0, min(a.counts[b], a.max_new)), a.capacity - T);
+    if (a.path) {  // max_new <= 64: a lane per entry
+        const int lane = threadIdx.x & 63;
+        const int at = lane < n ? a.path[(size_t)b * a.max_new + lane] : 0;
+        const uint64_t off = __ballot(at < 0 || at >= a.n_src);
+        if (off) n = min(n, __ffsll((long long)off) - 1);
+    }
+    return n;
+}
+
+// One workgroup: the 128-token group u of the groups that sequence b's new
+// tokens fall into (0 is the open one), of kv head h, of K (which 0) or V (1).
+// Thread (tr = tid / 16, m = tid % 16) owns dims 8 m .. + 7 of the group's
+// tokens tr, tr + 16, ..., so that a token's row is 16 lanes and every load and
+// store of a wavefront covers whole rows.
+__global__ __launch_bounds__(kThreads) void append_kernel(AppendArgs a) {
+    const int h = blockIdx.x >> 1, which = blockIdx.x & 1;
+    const int u = blockIdx.y, b = blockIdx.z;
+    const int tid = threadIdx.x, m = tid & 15, tr = tid >> 4, wave = tid >> 6;
+    const int Hkv = a.geo.Hkv;
+    const int T = min(max(a.seq_lens[b], 0), a.capacity);
+    const int n_new = appended(a, b, T);
+    const int end = T + n_new;
+    const int g0 = T / kKGroup, g = g0 + u;
+    const int t0 = g * kKGroup;
+    if (n_new == 0 || t0 >= end) return;
+    const int n = min(kKGroup, end - t0);  // tokens of the group
+    const int n_old = max(0, T - t0);      // of them in the cache already
+
+    const int32_t *bt_row = a.block_table + (size_t)b * a.geo.max_blocks;
+    const uint16_t *src = which == 0 ? a.k_new : a.v_new;
+    const size_t row_stride = (size_t)Hkv * kHeadDim;
+    const uint16_t *fresh = src + (size_t)b * a.n_src * row_stride + (size_t)h * kHeadDim + 8 * m;
+    uint16_t *ring = a.k_open + (size_t)b * kRing * row_stride + (size_t)h * kHeadDim + 8 * m;
+    auto new_row = [&](int t) {  // the new row of token t >= T
+        const int i = t - T;
+        return fresh + (size_t)(a.path ? a.path[(size_t)b * a.max_new + i] : i) * row_stride;
+    };
+
+    if (which == 1) {
+#pragma unroll
+        for (int i = 0; i < 8; ++i) {
+            const int tl = tr + 16 * i;
+            if (tl < n_old || tl >= n) continue;  // the same for a token's 16 lanes
+            const int t = t0 + tl;
+            float x[8];
+            unpack8(*reinterpret_cast<const uint4 *>(new_row(t)), x);
+            const float mn = row16_min(fmin3(fmin3(x[0], x[1], x[2]), fmin3(x[3], x[4], x[5]), fmin2(x[6], x[7])));
+            const float mx = row16_max(fmax3(fmax3(x[0], x[1], x[2]), fmax3(x[3], x[4], x[5]), fmax2(x[6], x[7])));
+            float zero, scale, inv;
+            group_params(mn, mx, zero, scale, inv);
+            if (m == 0) {
+                const size_t mi = ((size_t)b * Hkv + h) * a.geo.max_tokens + t;
+                a.meta.v_scale[mi] = scale;
+                a.meta.v_zero[mi] = zero;
+            }
+            const long long row = pool_row(a.geo, bt_row, a.bt_shift, h, t);
+            if (row < 0) continue;
+            const float z8[8] = {zero, zero, zero, zero, zero, zero, zero, zero};
+            const float i8[8] = {inv, inv, inv, inv, inv, inv, inv, inv};
+            store_codes(a, 1, x, z8, i8, row, m);
+        }
+        return;
+    }
+
+    __shared__ float s_min[4][kHeadDim], s_max[4][kHeadDim];
+    __shared__ float s_zero[kHeadDim], s_inv[kHeadDim];
+    uint4 raw[8];
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int tl = min(tr + 16 * i, n - 1);  // rows past the group's last repeat it
+        const uint16_t *p = tl < n_old ? ring + (size_t)((t0 + tl) % kRing) * row_stride : new_row(t0 + tl);
+        raw[i] = *reinterpret_cast<const uint4 *>(p);
+    }
+    float kmin[8], kmax[8];
+    {
+        float x[8][8];
+#pragma unroll
+        for (int i = 0; i < 8; ++i) unpack8(raw[i], x[i]);
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            kmin[j] = min_kg(fmin3(fmin3(x[0][j], x[1][j], x[2][j]), fmin3(x[3][j], x[4][j], x[5][j]),
+                                   fmin2(x[6][j], x[7][j])));
+            kmax[j] = max_kg(fmax3(fmax3(x[0][j], x[1][j], x[2][j]), fmax3(x[3][j], x[4][j], x[5][j]),
+                                   fmax2(x[6][j], x[7][j])));
+        }
+    }
+    if ((tid & 63) < 16) {
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            s_min[wave][8 * m + j] = kmin[j];
+            s_max[wave][8 * m + j] = kmax[j];
+        }
+    }
+    __syncthreads();  // every row that this workgroup reads from the ring is in registers
+    if (tid < kHeadDim) {
+        const float mn = fmin2(fmin2(s_min[0][tid], s_min[1][tid]), fmin2(s_min[2][tid], s_min[3][tid]));
+        const float mx = fmax2(fmax2(s_max[0][tid], s_max[1][tid]), fmax2(s_max[2][tid], s_max[3][tid]));
+        float zero, scale, inv;
+        group_params(mn, mx, zero, scale, inv);
+        s_zero[tid] = zero;
+        s_inv[tid] = inv;
+        const size_t mi = (((size_t)b * Hkv + h) * a.geo.n_groups + g) * kHeadDim + tid;
+        a.meta.k_scale[mi] = scale;
+        a.meta.k_zero[mi] = zero;
+    }
+    __syncthreads();
+    float kz[8], ki[8];
+#pragma unroll
+    for (int j = 0; j < 8; ++j) {
+        kz[j] = s_zero[8 * m + j];
+        ki[j] = s_inv[8 * m + j];
+    }
+#pragma unroll
+    for (int i = 0; i < 8; ++i) {
+        const int tl = tr + 16 * i;
+        if (tl >= n) continue;
+        const long long row = pool_row(a.geo, bt_row, a.bt_shift, h, t0 + tl);
+        if (row < 0) continue;
+        float x[8];
+        unpack8(raw[i], x);
+        store_codes(a, 0, x, kz, ki, row, m);
+    }
+
+    // ---- the ring: the rows of the last group begun, ge, and of the one before
+    // it.  Group g's rows stand in the half g % 2, which the open group's
+    // workgroup (u = 0) reads while the others run: a later group of the same
+    // half is left to that workgroup, which has its rows by now. ----
+    const int ge = end / kKGroup;
+    const bool old_rows = T % kKGroup != 0;  // the open group has rows in the ring
+    auto keep = [&](int group) {
+        for (int tl = tr; tl < kKGroup; tl += 16) {
+            const int t = group * kKGroup + tl;
+            if (t < T || t >= end) continue;
+            *reinterpret_cast<uint4 *>(ring + (size_t)(t % kRing) * row_stride) =
+                *reinterpret_cast<const uint4 *>(new_row(t));
+        }
+    };
+    if (g >= ge - 1 && (u == 0 || !old_rows || ((g ^ g0) & 1))) keep(g);
+    if (u == 0 && old_rows)
+        for (int later = max(g0 + 2, ge - 1); later <= ge; ++later)
+            if (((later ^ g0) & 1) == 0) keep(later);
+}
+
+// Reads tokens back: x = fma(code, scale, zero), rounded to BF16 to nearest
+// even.  A workgroup per (128-token K group, kv head, K or V), the K scales and
+// zeros of its 8 dims in a thread's registers for all of the group's tokens.
+// RING: K alone, the open group and the one before it, into the ring; else
+// tokens starts[b] .. + counts[b] - 1, to row t - starts[b] of the output.
+template <bool RING>
+__global__ __launch_bounds__(kThreads) void dequant_kernel(DequantArgs a) {
+    const int h = RING ? blockIdx.x : blockIdx.x >> 1, which = RING ? 0 : blockIdx.x & 1;
+    const int u = blockIdx.y, b = blockIdx.z;
+    const int tid = threadIdx.x, m = tid & 15, tr = tid >> 4;
+    const int Hkv = a.geo.Hkv;
+    int first, end;
+    if (RING) {
+        end = min(max(a.starts[b], 0), a.capacity);  // the sequence's length
+        first = max(0, end / kKGroup - 1) * kKGroup;
+    } else {
+        first = a.starts[b];
+        if (first < 0 || first >= a.capacity) return;
+        end = first + min(max(0, min(a.counts[b], a.max_n)), a.capacity - first);
+    }
+    const int g = first / kKGroup + u;
+    const int lo = max(first, g * kKGroup), hi = min(end, (g + 1) * kKGroup);
+    if (lo >= hi) return;
+    const int32_t *bt_row = a.block_table + (size_t)b * a.geo.max_blocks;
+    const uint8_t *codes = which == 0 ? a.k_codes : a.v_codes;
+    uint16_t *out = which == 0 ? a.k_out : a.v_out;
+    const int rows = RING ? kRing : a.max_n;
+    float sc[8], zr[8];
+    if (which == 0) {
+        const size_t km = (((size_t)b * Hkv + h) * a.geo.n_groups + g) * kHeadDim + 8 * m;
+#pragma unroll
+        for (int j = 0; j < 8; ++j) {
+            sc[j] = a.meta.k_scale[km + j];
+            zr[j] = a.meta.k_zero[km + j];
+        }
+    }
+    for (int t = lo + tr; t < hi; t += 16) {
+        const long long row = pool_row(a.geo, bt_row, a.bt_shift, h, t);
+        if (row < 0) continue;
+        const uint2 c = *reinterpret_cast<const uint2 *>(codes + row * kCodeRow + 8 * m);
+        if (which == 1) {
+            const size_t vm = ((size_t)b * Hkv + h) * a.geo.max_tokens + t;
+            const float s = a.meta.v_scale[vm], z = a.meta.v_zero[vm];
+#pragma unroll
+            for (int j = 0; j < 8; ++j) {
+                sc[j] = s;
+                zr[j] = z;
+            }
+        }
+        uint32_t o[4];
+#pragma unroll
+        for (int j = 0; j < 8; j += 2) {
+            const uint32_t w = (j < 4 ? c.x : c.y) >> (8 * (j & 3));
+            o[j / 2] = f32_to_bf16_bits(fmaf((float)(w & 0xFFu), sc[j], zr[j])) |
+                       (f32_to_bf16_bits(fmaf((float)((w >> 8) & 0xFFu), sc[j + 1], zr[j + 1])) << 16);
+        }
+        const size_t to = RING ? (size_t)(t % kRing) : (size_t)(t - first);
+        *reinterpret_cast<uint4 *>(out + (((size_t)b * rows + to) * Hkv + h) * kHeadDim + 8 * m) =
+            make_uint4(o[0], o[1], o[2], o[3]);
+    }
+}
+
+}  // namespace
+
+hipError_t launch_append(const AppendArgs &a, int B, hipStream_t stream) {
+    // groups that max_new tokens can touch, whatever the length before
+    const unsigned units = (unsigned)((a.max_new + 2 * kKGroup - 2) / kKGroup);
+    hipLaunchKernelGGL(append_kernel, dim3(2 * a.geo.Hkv, units, B), dim3(kThreads), 0, stream, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_dequant(const DequantArgs &a, int B, hipStream_t stream) {
+    const unsigned units = (unsigned)((a.max_n + 2 * kKGroup - 2) / kKGroup);
+    hipLaunchKernelGGL(dequant_kernel<false>, dim3(2 * a.geo.Hkv, units, B), dim3(kThreads), 0, stream, a);
+    return hipGetLastError();
+}
+
+hipError_t launch_append_begin(const DequantArgs &a, int B, hipStream_t stream) {
+    hipLaunchKernelGGL(dequant_kernel<true>, dim3(a.geo.Hkv, 2, B), dim3(kThreads), 0, stream, a);
+    return hipGetLastError();
+}
+
+}  // namespace lynx

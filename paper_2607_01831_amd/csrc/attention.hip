@@ -521,6 +521,68 @@ static void launch_combine_rows(int find, const AttnArgs &a, uint16_t *out, floa
         hipLaunchKernelGGL((attn_combine_rows_kernel<ROWS, 2>), grid, block, 0, stream, a, out, lse);
 }
 
+static VerifyArgs verify_args(const Geometry &g, const AttnPlan &plan, int B, int Hq, int nq, int max_seq_len,
+                              const int32_t *seq_lens, const int32_t *block_table, const uint8_t *k_codes,
+                              const uint8_t *v_codes, MetaPtrs meta, const uint16_t *q, float *ws_o, float2 *ws_ml) {
+    VerifyArgs v;
+    v.geo = g;
+    v.B = B;
+    v.Hq = Hq;
+    v.G = Hq / g.Hkv;
+    v.nq = nq;
+    v.max_seq_len = max_seq_len;
+    v.rows_total = plan.rows_total;
+    v.direct = plan.direct;
+    v.workers = plan.workers;
+    v.n_seg = plan.n_seg;
+    v.bt_shift = -1;
+    for (int sh = 0; sh < 31; ++sh)
+        if ((1 << sh) == g.bt) v.bt_shift = sh;
+    v.seq_lens = seq_lens;
+    v.block_table = block_table;
+    v.k_codes = k_codes;
+    v.v_codes = v_codes;
+    v.meta = meta;
+    v.q = q;
+    v.ws_o = ws_o;
+    v.ws_ml = ws_ml;
+    return v;
+}
+
+hipError_t launch_verify_tree(const Geometry &g, const AttnPlan &plan, int B, int Hq, int n, int max_seq_len,
+                              const int32_t *seq_lens, const int32_t *block_table, const uint8_t *k_codes,
+                              const uint8_t *v_codes, MetaPtrs meta, const uint16_t *q, const uint16_t *k_new,
+                              const uint16_t *v_new, const int32_t *parents, uint16_t *out, void *workspace,
+                              hipStream_t stream) {
+    float *ws_o = reinterpret_cast<float *>(reinterpret_cast<char *>(workspace) + kCounterBytes);
+    float2 *ws_ml = reinterpret_cast<float2 *>(reinterpret_cast<char *>(workspace) + kCounterBytes + plan.o_bytes);
+    hipError_t e = launch_verify_mfma(verify_args(g, plan, B, Hq, n, max_seq_len, seq_lens, block_table, k_codes,
+                                                  v_codes, meta, q, ws_o, ws_ml),
+                                      stream);
+    if (e != hipSuccess) return e;
+    TreeArgs a;
+    a.geo = g;
+    a.B = B;
+    a.Hq = Hq;
+    a.G = Hq / g.Hkv;
+    a.n = n;
+    a.max_seq_len = max_seq_len;
+    a.rows_total = plan.rows_total;
+    a.direct = plan.direct;
+    a.workers = plan.workers;
+    a.n_seg = plan.n_seg;
+    a.max_live = plan.max_live;
+    a.seq_lens = seq_lens;
+    a.parents = parents;
+    a.q = q;
+    a.k_new = k_new;
+    a.v_new = v_new;
+    a.ws_o = ws_o;
+    a.ws_ml = ws_ml;
+    a.out = out;
+    return launch_tree_combine(a, stream);
+}
+
 hipError_t launch_attention(KvMode mode, const Geometry &g, const AttnPlan &plan, int B, int Hq,
                             int nq, int max_seq_len, const int32_t *seq_lens,
                             const int32_t *block_table, const uint8_t *k_plane,
@@ -626,29 +688,9 @@ hipError_t launch_attention(KvMode mode, const Geometry &g, const AttnPlan &plan
         if (d.fused) return hipSuccess;
     } else if (mode == KvMode::kCodes) {
         // matrix-core verification over the context ...
-        VerifyArgs v;
-        v.geo = g;
-        v.B = B;
-        v.Hq = Hq;
-        v.G = a.G;
-        v.nq = nq;
-        v.max_seq_len = max_seq_len;
-        v.rows_total = plan.rows_total;
-        v.direct = plan.direct;
-        v.workers = plan.workers;
-        v.n_seg = plan.n_seg;
-        v.bt_shift = -1;
-        for (int sh = 0; sh < 31; ++sh)
-            if ((1 << sh) == g.bt) v.bt_shift = sh;
-        v.seq_lens = seq_lens;
-        v.block_table = block_table;
-        v.k_codes = k_plane;
-        v.v_codes = v_plane;
-        v.meta = meta;
-        v.q = q;
-        v.ws_o = a.ws_o;
-        v.ws_ml = a.ws_ml;
-        hipError_t e = launch_verify_mfma(v, stream);
+        hipError_t e = launch_verify_mfma(verify_args(g, plan, B, Hq, nq, max_seq_len, seq_lens, block_table, k_plane,
+                                                      v_plane, meta, q, a.ws_o, a.ws_ml),
+                                          stream);
         if (e != hipSuccess) return e;
         // the BF16 draft tail is attended by the combine kernel below
     } else {

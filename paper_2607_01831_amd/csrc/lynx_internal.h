@@ -226,6 +226,85 @@ hipError_t launch_attention(KvMode mode, const Geometry &g, const AttnPlan &plan
                             uint16_t *out, float *lse, void *workspace, hipStream_t stream,
                             int anchor_bits = 4);
 
+// ---- verification of a token tree (attention.hip, tree.hip) --------------------
+// Arguments of the merge of a tree's context partials with its own nodes.
+struct TreeArgs {
+    Geometry geo;
+    int B, Hq, G, n, max_seq_len;  // n nodes per sequence (<= 64)
+    int rows_total, direct, workers, n_seg, max_live;  // as in AttnPlan
+    const int32_t *seq_lens;
+    const int32_t *parents;        // [B][n]
+    const uint16_t *q;             // BF16 [B][n][Hq][128]
+    const uint16_t *k_new, *v_new; // BF16 [B][n][Hkv][128]
+    const float *ws_o;
+    const float2 *ws_ml;
+    uint16_t *out;                 // BF16 [B][n][Hq][128]
+};
+
+hipError_t launch_tree_combine(const TreeArgs &args, hipStream_t stream);
+// The tree's rows over the context (plan_attention of KvMode::kCodes with n
+// queries), then the merge.
+hipError_t launch_verify_tree(const Geometry &g, const AttnPlan &plan, int B, int Hq, int n, int max_seq_len,
+                              const int32_t *seq_lens, const int32_t *block_table, const uint8_t *k_codes,
+                              const uint8_t *v_codes, MetaPtrs meta, const uint16_t *q, const uint16_t *k_new,
+                              const uint16_t *v_new, const int32_t *parents, uint16_t *out, void *workspace,
+                              hipStream_t stream);
+
+// ---- the cache written token by token, and read back (append.hip) --------------
+// BF16 K rows kept per sequence behind its end (lynx.h's LYNX_OPEN_ROWS): the
+// open 128-token group's and the one's before it.
+constexpr int kOpenRows = 256;
+
+struct AppendArgs {
+    Geometry geo;
+    int max_new, n_src;       // tokens appended at most; rows of k_new per sequence
+    int capacity;             // tokens a sequence may hold
+    int bt_shift;             // log2(block_tokens) when it is a power of two, else -1
+    const int32_t *seq_lens;  // [B], before the append
+    const int32_t *counts;    // [B]
+    const int32_t *path;      // [B][max_new] rows of k_new, or nullptr: row i
+    const int32_t *block_table;
+    const uint16_t *k_new, *v_new;  // BF16 [B][n_src][Hkv][128]
+    uint16_t *k_open;               // BF16 [B][kOpenRows][Hkv][128]
+    uint8_t *codes[2], *anc[2], *res[2];  // planes of K and V, or nullptr
+    MetaPtrs meta;
+};
+
+struct DequantArgs {
+    Geometry geo;
+    int max_n;                // rows of the output per sequence
+    int capacity;
+    int bt_shift;
+    const int32_t *starts;    // [B]; append_begin: the lengths
+    const int32_t *counts;    // [B]
+    const int32_t *block_table;
+    const uint8_t *k_codes, *v_codes;
+    MetaPtrs meta;
+    uint16_t *k_out, *v_out;  // BF16 [B][max_n][Hkv][128]
+};
+
+hipError_t launch_append(const AppendArgs &args, int B, hipStream_t stream);
+hipError_t launch_dequant(const DequantArgs &args, int B, hipStream_t stream);
+hipError_t launch_append_begin(const DequantArgs &args, int B, hipStream_t stream);
+
+// ---- acceptance of a token tree (spec_tree.hip) ---------------------------------
+struct TreeAcceptArgs {
+    int n, vocab;
+    const float *scores;     // [B][n + 1][vocab]: logits, or probabilities where uniforms are given
+    const int32_t *tokens;   // [B][n]
+    const int32_t *parents;  // [B][n]
+    const float *uniforms;   // [B][n + 1], or nullptr: greedy
+    int32_t *accepted;       // [B]
+    int32_t *path;           // [B][n]
+    int32_t *next_token;     // [B]
+    // filled by the launch
+    int chunks;
+    uint32_t *part;   // [B][n + 1][chunks] pairs
+    int32_t *choice;  // [B][n + 1]
+};
+size_t spec_tree_workspace(int B, int n, int vocab);
+hipError_t launch_spec_accept_tree(TreeAcceptArgs args, int B, void *workspace, hipStream_t stream);
+
 // ---- acceptance of drafts (spec.hip) ------------------------------------------
 // Sampled acceptance workspace: B * (k + 1) * spec_accept_chunks(vocab) pairs of
 // uint64 chunk sums.

@@ -1,0 +1,190 @@
+"""Verification attention of a token tree (lynx_attn_verify_tree) against the
+plain fp64 statement over the same codes: head layouts, lengths from none to
+several thousand, trees of 1 to 64 nodes, padded and malformed trees, values
+that must not cross branches, other streams, graphs, shared workspaces.
+
+Tolerance, from the arithmetic: the output's rounding to BF16 is at most 2^-8
+of it.  A softmax weight over the context is rounded to fp16 (2^-11 of it) and
+multiplies s c, at most the range of V, so the output moves by at most 2^-11
+range.  A score is off by at most 2^-21 sum_d |q_d s_d c_d| / sqrt(128) (the
+query in two fp16 parts, 2^-22, and the fp32 sums): with |q s c| <= 64 a dim
+that is below 3.5e-4, and a weight then off by 3.5e-4 of it, the output by 3.5e-4
+range.  The range of V is below 10 here (N(0, 1) values), and of the node's own
+values too: 10 (2^-11 + 3.5e-4) = 8.4e-3."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import tree
+from paper_2607_01831_amd import lynx
+from tests._util import assert_close
+from tests.gpu_cases import bits, build_cache, device_meta_to_oracle, note, random_bf16, random_kv
+
+pytestmark = pytest.mark.gpu
+
+ATOL, RTOL = 8.4e-3, 2.0 ** -8 * 1.01
+
+
+def random_parents(B, n, seed, chain=0.5):
+    r = np.random.default_rng(seed)
+    return np.array([[-1 if i == 0 or r.random() < 0.15 else i - 1 if r.random() < chain else r.integers(0, i)
+                      for i in range(n)] for _ in range(B)], np.int32)
+
+
+def cache(lens, Hkv, bt=None, seed=0):
+    kv = [random_kv(T, Hkv, seed=seed + b) for b, T in enumerate(lens)]
+    return build_cache([k for k, _ in kv], [v for _, v in kv], Hkv, bt=bt, seed=seed, with_oracle=False)
+
+
+def inputs_of(c, Hq, n, seed=7):
+    return (random_bf16((c.B, n, Hq, 128), seed), random_bf16((c.B, n, c.Hkv, 128), seed + 1),
+            random_bf16((c.B, n, c.Hkv, 128), seed + 2))
+
+
+def run(c, q, kn, vn, parents, out=None, ws=None, max_len=None):
+    B, n, Hq, _ = q.shape
+    max_len = max(c.lens) if max_len is None else max_len
+    out = torch.full((B, n, Hq, 128), 7.0, dtype=torch.bfloat16, device="cuda") if out is None else out
+    ws = lynx.workspace(c.L, B, Hq, n, max_len) if ws is None else ws
+    note(f"verify_tree B={B} n={n} Hq={Hq} Hkv={c.Hkv} bt={c.bt} lens={c.lens[:4]}")
+    lynx.lynx_attn_verify_tree(c.L, B, Hq, n, max_len, c.lens_dev(), c.table_dev(), c.pool.k_codes, c.pool.v_codes,
+                               c.pool.meta, q.cuda(), kn.cuda(), vn.cuda(),
+                               torch.as_tensor(np.asarray(parents, np.int32)).cuda(), out, ws)
+    torch.cuda.synchronize()
+    return out.float().cpu().numpy()
+
+
+def want(c, q, kn, vn, parents, lens=None):
+    return tree.verify_tree(c.OL, q.shape[2], c.lens if lens is None else lens, c.table.numpy(),
+                            c.pool.k_codes.cpu().numpy(), c.pool.v_codes.cpu().numpy(), device_meta_to_oracle(c), bits(q),
+                            bits(kn), bits(vn), parents)
+
+
+@pytest.mark.parametrize("lens,Hkv,G,n,bt", [
+    ([1], 1, 1, 1, None),
+    ([0], 2, 4, 5, None),               # no context: the tree alone
+    ([300], 1, 7, 2, None),
+    ([4096], 4, 2, 8, None),
+    ([2049], 2, 4, 64, None),           # rows past one tile
+    ([700, 0, 129, 1500], 2, 4, 17, 16),
+    ([640, 1, 513], 2, 8, 25, 24),      # blocks that are no multiple of 16 tokens
+    ([900, 31], 1, 16, 63, 48),
+    ([130, 257], 3, 3, 33, 1),          # a token a block
+    ([1200] * 5, 2, 1, 9, 64),
+    ([20000], 1, 4, 12, None),          # many partials a row
+    ([64] * 70, 1, 2, 3, 16),           # more sequences than lanes
+])
+def test_trees(lens, Hkv, G, n, bt):
+    c = cache(lens, Hkv, bt)
+    x = inputs_of(c, Hkv * G, n)
+    parents = random_parents(c.B, n, seed=n)
+    assert_close(run(c, *x, parents), want(c, *x, parents), ATOL, RTOL, "tree")
+
+
+def test_a_chain_is_the_linear_verification():
+    c = cache([777, 2000], 2, 16)
+    q, kn, vn = inputs_of(c, 8, 11)
+    chain = np.tile(np.arange(11) - 1, (2, 1))
+    out = torch.empty(2, 11, 8, 128, dtype=torch.bfloat16, device="cuda")
+    ws = lynx.workspace(c.L, 2, 8, 11, 2000)
+    note("verify chain")
+    lynx.lynx_attn_verify(c.L, 2, 8, 11, 2000, c.lens_dev(), c.table_dev(), c.pool.k_codes, c.pool.v_codes, c.pool.meta,
+                          q.cuda(), kn.cuda(), vn.cuda(), out, ws)
+    torch.cuda.synchronize()
+    # the same context partials; the tail's sums and the two roundings to BF16 apart
+    assert_close(run(c, q, kn, vn, chain), out.float().cpu().numpy(), 1e-3, 2.0 ** -7, "chain")
+
+
+def test_padded_and_malformed_trees():
+    """Nodes that are not there: padding (-2), a parent at or behind the node or
+    far outside, everything below such a node, and a sequence of none."""
+    c = cache([500, 333, 64], 2, 16)
+    x = inputs_of(c, 8, 8)
+    parents = np.array([[-1, 0, -2, 2, 1, 5, 9, 2 ** 30], [0, -1, 1, -2 ** 31, 3, 2, 5, -2], [-2] * 8], np.int32)
+    got, ref = run(c, *x, parents), want(c, *x, parents)
+    assert_close(got, ref, ATOL, RTOL, "padded")
+    for b, i in [(0, 2), (0, 3), (0, 5), (0, 6), (0, 7), (1, 0), (1, 3), (1, 4), (1, 7)] + [(2, i) for i in range(8)]:
+        assert (got[b, i] == 0).all(), (b, i)
+
+
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), -float("inf"), 3e38])
+@pytest.mark.parametrize("n", [6, 40])
+def test_values_stay_on_their_path(value, n):
+    """K and V of a node reach its descendants and itself alone."""
+    c = cache([260, 40], 2, 16)
+    q, kn, vn = inputs_of(c, 8, n)
+    parents = random_parents(2, n, seed=1)
+    parents[:, :4] = [[-1, -1, 0, 1], [-1, 0, 0, 1]]
+    parents[:, -1] = -2  # not there
+    clean = run(c, q, kn, vn, parents)
+    bad = 1
+    dirty_k, dirty_v = kn.clone(), vn.clone()
+    for x in (dirty_k, dirty_v):
+        x[:, bad] = value
+        x[:, -1] = value
+    got = run(c, q, dirty_k, dirty_v, parents)
+    for b in range(2):
+        for i, seen in enumerate(tree.ancestors(parents[b])):
+            if seen is None or bad not in seen:
+                assert np.array_equal(got[b, i], clean[b, i]), (b, i)
+
+
+def test_a_dominant_node_and_a_dominant_context():
+    """Scores that leave one side no weight."""
+    c = cache([1000], 2)
+    q, kn, vn = inputs_of(c, 8, 9)
+    parents = random_parents(1, 9, seed=5)
+    for scale in (0.01, 30.0):
+        x = (q * (4 if scale > 1 else 1), kn * scale, vn)
+        assert_close(run(c, *x, parents), want(c, *x, parents), ATOL, RTOL, f"x{scale}")
+
+
+def test_lengths_past_the_bound_and_bad_blocks():
+    c = cache([600, 700], 2, 16)
+    x = inputs_of(c, 8, 5)
+    parents = random_parents(2, 5, seed=2)
+    assert_close(run(c, *x, parents, max_len=512), want(c, *x, parents, lens=[512, 512]), ATOL, RTOL, "bound")
+    c.table = c.table.clone()
+    c.table[1, 3] = c.n_blocks  # of sequence 1 alone
+    parents[1, 4] = -2
+    got = run(c, *x, parents)
+    assert np.isfinite(got[0]).all() and np.isnan(got[1, :4]).all() and (got[1, 4] == 0).all()
+
+
+def test_another_stream_a_shared_workspace_and_a_graph():
+    """One workspace for calls of several shapes, eager and in two graphs whose
+    replays alternate with the eager calls."""
+    shapes = [cache([900, 100], 2, 16, seed=1), cache([3000], 4, None, seed=2)]
+    work = []
+    for c, (Hq, n) in zip(shapes, ((8, 30), (16, 7))):
+        x = inputs_of(c, Hq, n)
+        parents = random_parents(c.B, n, seed=3)
+        work.append([c, x, parents, run(c, *x, parents)])
+    size = max(lynx.lynx_attn_workspace_bytes(c.L, c.B, x[0].shape[2], x[0].shape[1], max(c.lens)) for c, x, _, _ in work)
+    ws = torch.zeros(size, dtype=torch.uint8, device="cuda")
+    graphs = []
+    side = torch.cuda.Stream()
+    for c, x, parents, _ in work:
+        dev = [t.cuda() for t in x] + [torch.as_tensor(parents).cuda()]
+        lens, table = c.lens_dev(), c.table_dev()
+        out = torch.empty(x[0].shape, dtype=torch.bfloat16, device="cuda")
+        args = (c.L, c.B, x[0].shape[2], x[0].shape[1], max(c.lens), lens, table, c.pool.k_codes, c.pool.v_codes, c.pool.meta,
+                *dev, out, ws)
+        torch.cuda.synchronize()
+        g = torch.cuda.CUDAGraph()
+        with torch.cuda.graph(g, stream=side):
+            lynx.lynx_attn_verify_tree(*args)
+        graphs.append((g, args, out))
+    for turn in range(3):
+        for (g, args, out), (c, x, parents, ref) in zip(graphs, work):
+            out.fill_(7)
+            note(f"replay {turn}")
+            g.replay()
+            torch.cuda.synchronize()
+            assert np.array_equal(out.float().cpu().numpy(), ref)
+            out.fill_(7)
+            torch.cuda.synchronize()
+            with torch.cuda.stream(side):
+                lynx.lynx_attn_verify_tree(*args)
+            side.synchronize()
+            assert np.array_equal(out.float().cpu().numpy(), ref)
