@@ -591,7 +591,8 @@ size_t lynx_spec_tree_workspace_bytes(int32_t B, int32_t n, int32_t vocab) {
 namespace {
 int accept_tree(int32_t B, int32_t n, int32_t vocab, const float *scores, const int32_t *tokens,
                 const int32_t *parents, const float *uniforms, int32_t *accepted, int32_t *path,
-                int32_t *next_token, void *workspace, size_t workspace_bytes, void *stream) {
+                int32_t *next_token, void *workspace, size_t workspace_bytes, void *stream,
+                const lynx::TreeAcceptWay *way = nullptr) {
     if (B < 0 || B > kMostB || n < 1 || n > 64 || vocab < 1 || vocab > (1 << 23)) return LYNX_EINVAL;
     if (B == 0) return LYNX_OK;
     const void *ptrs[] = {scores, tokens, parents, accepted, path, next_token};
@@ -609,7 +610,8 @@ int accept_tree(int32_t B, int32_t n, int32_t vocab, const float *scores, const 
     a.accepted = accepted;
     a.path = path;
     a.next_token = next_token;
-    hipError_t e = lynx::launch_spec_accept_tree(a, B, workspace, static_cast<hipStream_t>(stream));
+    hipError_t e = lynx::launch_spec_accept_tree(a, B, way ? *way : lynx::spec_tree_way(B, n, vocab, uniforms != nullptr),
+                                                 workspace, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? LYNX_OK : LYNX_EHIP;
 }
 }  // namespace
@@ -630,6 +632,18 @@ int lynx_spec_accept_tree_sample(int32_t B, int32_t n, int32_t vocab, const floa
     if (B > 0 && (!uniforms || !aligned16(uniforms))) return LYNX_EINVAL;
     return accept_tree(B, n, vocab, target_probs, tokens, parents, uniforms, accepted, path, next_token, workspace,
                        workspace_bytes, stream);
+}
+
+// Not in lynx.h: the acceptance calls with their way of reading the rows given
+// (uniforms NULL: greedy), so that tests reach every one of them, with waits that
+// end at once too.
+int lynx_internal_accept_tree(int32_t B, int32_t n, int32_t vocab, const float *scores, const int32_t *tokens,
+                              const int32_t *parents, const float *uniforms, int32_t *accepted, int32_t *path,
+                              int32_t *next_token, void *workspace, size_t workspace_bytes, int32_t rows,
+                              int32_t looks, void *stream) {
+    const lynx::TreeAcceptWay way{rows != 0, looks};
+    return accept_tree(B, n, vocab, scores, tokens, parents, uniforms, accepted, path, next_token, workspace,
+                       workspace_bytes, stream, &way);
 }
 
 int lynx_kv_append(const lynx_layout *L, int32_t B, int32_t max_new, int32_t n_src, const int32_t *seq_lens,

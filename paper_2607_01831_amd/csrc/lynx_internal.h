@@ -288,6 +288,7 @@ hipError_t launch_dequant(const DequantArgs &args, int B, hipStream_t stream);
 hipError_t launch_append_begin(const DequantArgs &args, int B, hipStream_t stream);
 
 // ---- acceptance of a token tree (spec_tree.hip) ---------------------------------
+constexpr int kTreeStateBytes = 64;
 struct TreeAcceptArgs {
     int n, vocab;
     const float *scores;     // [B][n + 1][vocab]: logits, or probabilities where uniforms are given
@@ -298,12 +299,18 @@ struct TreeAcceptArgs {
     int32_t *path;           // [B][n]
     int32_t *next_token;     // [B]
     // filled by the launch
-    int chunks;
-    uint32_t *part;   // [B][n + 1][chunks] pairs
-    int32_t *choice;  // [B][n + 1]
+    int chunks;       // of the vocabulary
+    int looks;        // at a row that is not in, before a workgroup stops waiting
+    void *state;      // [B][n + 2] states of kTreeStateBytes
+    uint64_t *words;  // [B][n + 1][chunks]
 };
 size_t spec_tree_workspace(int B, int n, int vocab);
-hipError_t launch_spec_accept_tree(TreeAcceptArgs args, int B, void *workspace, hipStream_t stream);
+struct TreeAcceptWay {
+    bool rows;  // every row at once, or along the path
+    int looks;
+};
+TreeAcceptWay spec_tree_way(int B, int n, int vocab, bool drawn);
+hipError_t launch_spec_accept_tree(TreeAcceptArgs args, int B, TreeAcceptWay way, void *workspace, hipStream_t stream);
 
 // ---- acceptance of drafts (spec.hip) ------------------------------------------
 // Sampled acceptance workspace: B * (k + 1) * spec_accept_chunks(vocab) pairs of

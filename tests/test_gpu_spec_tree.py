@@ -1,5 +1,7 @@
 """Acceptance of a token tree, greedy and drawn, against the plain walk: whole
 numbers, equal in every place."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -24,6 +26,24 @@ def run(scores, tokens, parents, uniforms=None, ws=None):
         lynx.lynx_spec_accept_tree_sample(*dev, torch.as_tensor(uniforms).cuda(), *out, ws)
     torch.cuda.synchronize()
     assert int(ws.max()) == 0  # left as it was found
+    return [x.cpu().numpy() for x in out]
+
+
+def run_way(scores, tokens, parents, uniforms, rows, looks):
+    """The same by a given way of reading the rows."""
+    B, n, V = *tokens.shape, scores.shape[2]
+    dev = [torch.as_tensor(np.ascontiguousarray(x)).cuda() for x in (scores, tokens.astype(np.int32), parents.astype(np.int32))]
+    u = None if uniforms is None else torch.as_tensor(uniforms).cuda()
+    out = [torch.full(s, -7, dtype=torch.int32, device="cuda") for s in ((B,), (B, n), (B,))]
+    ws = lynx.spec_tree_workspace(B, n, V)
+    f = lynx.load().lynx_internal_accept_tree
+    P, I = ctypes.c_void_p, ctypes.c_int32
+    f.argtypes = [I, I, I, P, P, P, P, P, P, P, P, ctypes.c_size_t, I, I, P]
+    note(f"accept_tree B={B} n={n} V={V} drawn={u is not None} rows={rows} looks={looks}")
+    assert f(B, n, V, *[x.data_ptr() for x in dev], None if u is None else u.data_ptr(), *[x.data_ptr() for x in out],
+             ws.data_ptr(), ws.nbytes, rows, looks, torch.cuda.current_stream().cuda_stream) == 0
+    torch.cuda.synchronize()
+    assert int(ws.max()) == 0
     return [x.cpu().numpy() for x in out]
 
 
@@ -55,9 +75,20 @@ def case(B, n, V, seed, drawn, agree=0.7):
 
 @pytest.mark.parametrize("drawn", [False, True])
 @pytest.mark.parametrize("B,n,V", [(1, 1, 1), (1, 1, 2), (3, 5, 7), (1, 64, 4095), (2, 63, 4096), (2, 17, 4097), (1, 8, 32000),
-                                   (4, 24, 50257), (300, 3, 33), (40, 64, 100), (16, 9, 8192), (1, 2, 128256)])
+                                   (4, 24, 50257), (300, 3, 33), (40, 64, 100), (16, 9, 8192), (1, 2, 128256), (12, 60, 50000)])
 def test_trees(B, n, V, drawn):
     check(*case(B, n, V, seed=B + n, drawn=drawn))
+
+
+@pytest.mark.parametrize("drawn", [False, True])
+@pytest.mark.parametrize("rows,looks", [(1, 0), (0, 128), (0, 1), (0, 0)])
+def test_every_way_of_reading_the_rows(rows, looks, drawn):
+    """All rows at once; along the path; along the path with workgroups that stop
+    waiting after one look or none, so that the last one walks."""
+    for i, (B, n, V) in enumerate([(1, 1, 1), (3, 5, 8193), (2, 64, 20001), (7, 33, 4096), (1, 9, 50257), (70, 6, 40)]):
+        c = case(B, n, V, 20 + i, drawn, agree=0.9)
+        for g, w in zip(run_way(*c, rows, looks), tree.accept_tree(*c)):
+            assert np.array_equal(g, w)
 
 
 @pytest.mark.parametrize("drawn", [False, True])
