@@ -8,6 +8,7 @@ library is missing the binding raises instead of falling back to anything.
 from __future__ import annotations
 
 import ctypes
+import struct
 from dataclasses import dataclass
 from pathlib import Path
 
@@ -88,13 +89,13 @@ def load():
         "lynx_kv_encode_split": ([LP, I32, I32, I32, P, P, P, P, P, P, P, MP, P], ctypes.c_int),
         "lynx_kv_merge_split": ([I32, SZ, P, P, P, P], ctypes.c_int),
         "lynx_kv_dequant_anchor_split": ([LP, I32, I32, I32, P, P, P, MP, P, P, P], ctypes.c_int),
-        "lynx_attn_verify_tree": ([LP, I32, I32, I32, I32, P, P, P, P, MP, P, P, P, P, P, P, SZ, P], ctypes.c_int),
+        "lynx_attn_verify_tree": ([P, I32, I32, I32, I32, P, P, P, P, P, P, P, P, P, P, P, SZ, P], ctypes.c_int),
         "lynx_spec_tree_workspace_bytes": ([I32, I32, I32], SZ),
         "lynx_spec_accept_tree_greedy": ([I32, I32, I32, P, P, P, P, P, P, P, SZ, P], ctypes.c_int),
         "lynx_spec_accept_tree_sample": ([I32, I32, I32, P, P, P, P, P, P, P, P, SZ, P], ctypes.c_int),
-        "lynx_kv_append": ([LP, I32, I32, I32, P, P, P, P, P, P, P, P, P, P, P, P, P, MP, P], ctypes.c_int),
-        "lynx_kv_append_begin": ([LP, I32, P, P, P, MP, P, P], ctypes.c_int),
-        "lynx_kv_dequant": ([LP, I32, I32, P, P, P, P, P, MP, P, P, P], ctypes.c_int),
+        "lynx_kv_append": ([P, I32, I32, I32, P, P, P, P, P, P, P, P, P, P, P, P, P, P, P], ctypes.c_int),
+        "lynx_kv_append_begin": ([P, I32, P, P, P, P, P, P], ctypes.c_int),
+        "lynx_kv_dequant": ([P, I32, I32, P, P, P, P, P, P, P, P, P], ctypes.c_int),
         "lynx_strerror": ([ctypes.c_int], ctypes.c_char_p),
     }
     for name, (args, res) in sigs.items():
@@ -189,25 +190,50 @@ def _attn_args(fn: str, L: "Layout", B: int, Hq: int, seq_lens, block_table, k_p
         ctypes.byref(_meta_arg(fn, L, meta, B)), _arg(fn, "q", q, B * nq * Hq * HEAD_DIM * 2))
 
 
-def _typed(fn: str, what: str, t, nbytes: int, dtype):
-    """_arg for a tensor of one type on the current device (planes are uint8,
-    counts and tables int32, metadata and scores fp32, K, V and q BF16)."""
-    if t is not None and not isinstance(t, int):
+def _here(stream):
+    """The current device and the stream of a call (without a CUDA context yet
+    there is no tensor to launch on)."""
+    if not torch.cuda.is_initialized():
+        return 0, stream
+    dev = torch._C._cuda_getDevice()
+    if stream is None:
+        return dev, torch._C._cuda_getCurrentRawStream(dev)
+    return dev, stream.cuda_stream if isinstance(stream, torch.cuda.Stream) else stream
+
+
+def _typed(fn: str, what: str, t, nbytes: int, dtype, dev: int):
+    """_arg for a contiguous tensor of one type on the call's device (planes are
+    uint8, counts and tables int32, metadata and scores fp32, K, V and q BF16).
+    A call makes up to 21 of these: one test where nothing is wrong (an append
+    14.7 -> 10 us on the host)."""
+    if t is None or t.__class__ is int:
+        return t
+    if t.dtype is not dtype or t.nbytes < nbytes or t.get_device() != dev or not t.is_contiguous():
         if t.dtype is not dtype:
-            raise ValueError(f"{fn}: {what} is {t.dtype}; the call reads {dtype}")
-        if t.is_cuda and t.get_device() != torch._C._cuda_getDevice():
-            raise ValueError(f"{fn}: {what} is on device {t.get_device()}, not on the current one")
-    return _arg(fn, what, t, nbytes)
+            raise ValueError(f"{fn}: {what} is {t.dtype}; the call uses {dtype}")
+        if t.is_cuda and t.get_device() != dev:
+            raise ValueError(f"{fn}: {what} is on device {t.get_device()}, not on the current one ({dev})")
+        _arg(fn, what, t, nbytes)  # raises for what is left
+    return t.data_ptr()
 
 
 _BF16, _F32, _I32, _U8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
+_pack_layout, _pack_meta = struct.Struct("7i").pack, struct.Struct("4P").pack
 
 
-def _typed_meta(fn: str, L: "Layout", meta: "Meta", rows: int) -> lynx_meta:
+def _packed(L: "Layout") -> bytes:
+    """The lynx_layout as bytes (a quarter of the time of the ctypes structure)."""
+    return _pack_layout(L.num_kv_heads, L.head_dim, L.k_group_tokens, L.block_tokens, L.max_blocks_per_seq,
+                        L.num_blocks, L.max_tokens)
+
+
+def _typed_meta(fn: str, L: "Layout", meta: "Meta", rows: int, dev: int) -> bytes:
     heads = rows * L.num_kv_heads
     k, v = heads * -(-L.max_tokens // K_GROUP) * HEAD_DIM * 4, heads * L.max_tokens * 4
-    return lynx_meta(_typed(fn, "meta.k_scale", meta.k_scale, k, _F32), _typed(fn, "meta.k_zero", meta.k_zero, k, _F32),
-                     _typed(fn, "meta.v_scale", meta.v_scale, v, _F32), _typed(fn, "meta.v_zero", meta.v_zero, v, _F32))
+    return _pack_meta(_typed(fn, "meta.k_scale", meta.k_scale, k, _F32, dev) or 0,
+                      _typed(fn, "meta.k_zero", meta.k_zero, k, _F32, dev) or 0,
+                      _typed(fn, "meta.v_scale", meta.v_scale, v, _F32, dev) or 0,
+                      _typed(fn, "meta.v_zero", meta.v_zero, v, _F32, dev) or 0)
 
 
 @dataclass
@@ -402,18 +428,18 @@ def lynx_attn_verify_tree(L: Layout, B: int, Hq: int, n: int, max_seq_len: int, 
                           workspace_buf=None, stream=None) -> None:
     """Verification of a tree: q [B][n][Hq][128], k_new and v_new
     [B][n][Hkv][128], parents int32 [B][n]; workspace() of n queries."""
-    fn = "lynx_attn_verify_tree"
+    fn, (dev, stream) = "lynx_attn_verify_tree", _here(stream)
     ws, nb, nn = workspace_buf, max(B, 0), max(n, 0)
     plane, kv = L.plane_bytes(128), nb * nn * L.num_kv_heads * HEAD_DIM * 2
     io = nb * nn * Hq * HEAD_DIM * 2
     _check(fn, load().lynx_attn_verify_tree(
-        ctypes.byref(L.c()), B, Hq, n, max_seq_len, _typed(fn, "seq_lens", seq_lens, nb * 4, _I32),
-        _typed(fn, "block_table", block_table, nb * L.max_blocks_per_seq * 4, _I32),
-        _typed(fn, "k_codes", k_codes, plane, _U8), _typed(fn, "v_codes", v_codes, plane, _U8),
-        ctypes.byref(_typed_meta(fn, L, meta, nb)), _typed(fn, "q", q, io, _BF16),
-        _typed(fn, "k_new", k_new, kv, _BF16), _typed(fn, "v_new", v_new, kv, _BF16),
-        _typed(fn, "parents", parents, nb * nn * 4, _I32), _typed(fn, "out", out, io, _BF16),
-        _typed(fn, "workspace_buf", ws, 0, _U8), 0 if ws is None else ws.nbytes, _stream(stream)))
+        _packed(L), B, Hq, n, max_seq_len, _typed(fn, "seq_lens", seq_lens, nb * 4, _I32, dev),
+        _typed(fn, "block_table", block_table, nb * L.max_blocks_per_seq * 4, _I32, dev),
+        _typed(fn, "k_codes", k_codes, plane, _U8, dev), _typed(fn, "v_codes", v_codes, plane, _U8, dev),
+        _typed_meta(fn, L, meta, nb, dev), _typed(fn, "q", q, io, _BF16, dev),
+        _typed(fn, "k_new", k_new, kv, _BF16, dev), _typed(fn, "v_new", v_new, kv, _BF16, dev),
+        _typed(fn, "parents", parents, nb * nn * 4, _I32, dev), _typed(fn, "out", out, io, _BF16, dev),
+        _typed(fn, "workspace_buf", ws, 0, _U8, dev), 0 if ws is None else ws.nbytes, stream))
 
 
 def lynx_spec_tree_workspace_bytes(B: int, n: int, vocab: int) -> int:
@@ -426,17 +452,17 @@ def spec_tree_workspace(B: int, n: int, vocab: int, device="cuda") -> torch.Tens
     return torch.zeros(max(lynx_spec_tree_workspace_bytes(B, n, vocab), 16), dtype=torch.uint8, device=device)
 
 
-def _tree_args(fn: str, scores, tokens, parents, accepted, path, next_token, uniforms=None):
+def _tree_args(fn: str, dev: int, scores, tokens, parents, accepted, path, next_token, uniforms=None):
     if scores.dim() != 3:
         raise ValueError(f"{fn}: the scores are [B][n + 1][vocab]")
     B, n1, V = (int(x) for x in scores.shape)
     rows = B * (n1 - 1) * 4
     return B, n1 - 1, V, [
-        _typed(fn, "scores", scores, B * n1 * V * 4, _F32), _typed(fn, "tokens", tokens, rows, _I32),
-        _typed(fn, "parents", parents, rows, _I32),
-        *([] if uniforms is None else [_typed(fn, "uniforms", uniforms, B * n1 * 4, _F32)]),
-        _typed(fn, "accepted", accepted, B * 4, _I32), _typed(fn, "path", path, rows, _I32),
-        _typed(fn, "next_token", next_token, B * 4, _I32)]
+        _typed(fn, "scores", scores, B * n1 * V * 4, _F32, dev), _typed(fn, "tokens", tokens, rows, _I32, dev),
+        _typed(fn, "parents", parents, rows, _I32, dev),
+        *([] if uniforms is None else [_typed(fn, "uniforms", uniforms, B * n1 * 4, _F32, dev)]),
+        _typed(fn, "accepted", accepted, B * 4, _I32, dev), _typed(fn, "path", path, rows, _I32, dev),
+        _typed(fn, "next_token", next_token, B * 4, _I32, dev)]
 
 
 def lynx_spec_accept_tree_greedy(target_logits, tokens, parents, accepted, path, next_token,
@@ -444,24 +470,24 @@ def lynx_spec_accept_tree_greedy(target_logits, tokens, parents, accepted, path,
     """target_logits fp32 [B][n+1][V], tokens and parents int32 [B][n]; writes
     accepted, next_token (int32 [B]) and path (int32 [B][n]).  workspace_buf:
     spec_tree_workspace(); None makes one for this call."""
-    fn = "lynx_spec_accept_tree_greedy"
-    B, n, V, args = _tree_args(fn, target_logits, tokens, parents, accepted, path, next_token)
+    fn, (dev, stream) = "lynx_spec_accept_tree_greedy", _here(stream)
+    B, n, V, args = _tree_args(fn, dev, target_logits, tokens, parents, accepted, path, next_token)
     ws = workspace_buf if workspace_buf is not None else spec_tree_workspace(B, n, V, target_logits.device)
-    _check(fn, load().lynx_spec_accept_tree_greedy(B, n, V, *args, _typed(fn, "workspace_buf", ws, 0, _U8), ws.nbytes,
-                                                   _stream(stream)))
+    _check(fn, load().lynx_spec_accept_tree_greedy(B, n, V, *args, _typed(fn, "workspace_buf", ws, 0, _U8, dev), ws.nbytes,
+                                                   stream))
 
 
 def lynx_spec_accept_tree_sample(target_probs, tokens, parents, uniforms, accepted, path, next_token,
                                  workspace_buf=None, stream=None) -> None:
     """target_probs fp32 [B][n+1][V], uniforms fp32 [B][n+1]; the rest as
     lynx_spec_accept_tree_greedy."""
-    fn = "lynx_spec_accept_tree_sample"
+    fn, (dev, stream) = "lynx_spec_accept_tree_sample", _here(stream)
     if uniforms is None:
         raise LynxError(fn, LYNX_EINVAL)
-    B, n, V, args = _tree_args(fn, target_probs, tokens, parents, accepted, path, next_token, uniforms)
+    B, n, V, args = _tree_args(fn, dev, target_probs, tokens, parents, accepted, path, next_token, uniforms)
     ws = workspace_buf if workspace_buf is not None else spec_tree_workspace(B, n, V, target_probs.device)
-    _check(fn, load().lynx_spec_accept_tree_sample(B, n, V, *args, _typed(fn, "workspace_buf", ws, 0, _U8), ws.nbytes,
-                                                   _stream(stream)))
+    _check(fn, load().lynx_spec_accept_tree_sample(B, n, V, *args, _typed(fn, "workspace_buf", ws, 0, _U8, dev), ws.nbytes,
+                                                   stream))
 
 
 # BF16 K rows kept per sequence for its open group (lynx.h).
@@ -473,48 +499,48 @@ def lynx_kv_append(L: Layout, B: int, max_new: int, seq_lens, counts, path, bloc
     """k_new, v_new: BF16 [B][n_src][Hkv][128]; path int32 [B][max_new] or None;
     k_open BF16 [B][OPEN_ROWS][Hkv][128]; pairs of planes that are not kept are
     None."""
-    fn = "lynx_kv_append"
+    fn, (dev, stream) = "lynx_kv_append", _here(stream)
     nb, row = max(B, 0), L.num_kv_heads * HEAD_DIM * 2
     if k_new.dim() != 4:
         raise ValueError(f"{fn}: k_new is [B][n_src][Hkv][128]")
     n_src = int(k_new.shape[1])
     codes, nibbles = L.plane_bytes(128), L.plane_bytes(64)
     _check(fn, load().lynx_kv_append(
-        ctypes.byref(L.c()), B, max_new, n_src, _typed(fn, "seq_lens", seq_lens, nb * 4, _I32),
-        _typed(fn, "counts", counts, nb * 4, _I32), _typed(fn, "path", path, nb * max(max_new, 0) * 4, _I32),
-        _typed(fn, "block_table", block_table, nb * L.max_blocks_per_seq * 4, _I32),
-        _typed(fn, "k_new", k_new, nb * n_src * row, _BF16), _typed(fn, "v_new", v_new, nb * n_src * row, _BF16),
-        _typed(fn, "k_open", k_open, nb * OPEN_ROWS * row, _BF16),
-        _typed(fn, "k_codes", k_codes, codes, _U8), _typed(fn, "v_codes", v_codes, codes, _U8),
-        _typed(fn, "k_anc", k_anc, nibbles, _U8), _typed(fn, "v_anc", v_anc, nibbles, _U8),
-        _typed(fn, "k_res", k_res, nibbles, _U8), _typed(fn, "v_res", v_res, nibbles, _U8),
-        ctypes.byref(_typed_meta(fn, L, meta, nb)), _stream(stream)))
+        _packed(L), B, max_new, n_src, _typed(fn, "seq_lens", seq_lens, nb * 4, _I32, dev),
+        _typed(fn, "counts", counts, nb * 4, _I32, dev), _typed(fn, "path", path, nb * max(max_new, 0) * 4, _I32, dev),
+        _typed(fn, "block_table", block_table, nb * L.max_blocks_per_seq * 4, _I32, dev),
+        _typed(fn, "k_new", k_new, nb * n_src * row, _BF16, dev), _typed(fn, "v_new", v_new, nb * n_src * row, _BF16, dev),
+        _typed(fn, "k_open", k_open, nb * OPEN_ROWS * row, _BF16, dev),
+        _typed(fn, "k_codes", k_codes, codes, _U8, dev), _typed(fn, "v_codes", v_codes, codes, _U8, dev),
+        _typed(fn, "k_anc", k_anc, nibbles, _U8, dev), _typed(fn, "v_anc", v_anc, nibbles, _U8, dev),
+        _typed(fn, "k_res", k_res, nibbles, _U8, dev), _typed(fn, "v_res", v_res, nibbles, _U8, dev),
+        _typed_meta(fn, L, meta, nb, dev), stream))
 
 
 def lynx_kv_append_begin(L: Layout, B: int, seq_lens, block_table, k_codes, meta: Meta, k_open,
                          stream=None) -> None:
-    fn = "lynx_kv_append_begin"
+    fn, (dev, stream) = "lynx_kv_append_begin", _here(stream)
     nb = max(B, 0)
     _check(fn, load().lynx_kv_append_begin(
-        ctypes.byref(L.c()), B, _typed(fn, "seq_lens", seq_lens, nb * 4, _I32),
-        _typed(fn, "block_table", block_table, nb * L.max_blocks_per_seq * 4, _I32),
-        _typed(fn, "k_codes", k_codes, L.plane_bytes(128), _U8), ctypes.byref(_typed_meta(fn, L, meta, nb)),
-        _typed(fn, "k_open", k_open, nb * OPEN_ROWS * L.num_kv_heads * HEAD_DIM * 2, _BF16), _stream(stream)))
+        _packed(L), B, _typed(fn, "seq_lens", seq_lens, nb * 4, _I32, dev),
+        _typed(fn, "block_table", block_table, nb * L.max_blocks_per_seq * 4, _I32, dev),
+        _typed(fn, "k_codes", k_codes, L.plane_bytes(128), _U8, dev), _typed_meta(fn, L, meta, nb, dev),
+        _typed(fn, "k_open", k_open, nb * OPEN_ROWS * L.num_kv_heads * HEAD_DIM * 2, _BF16, dev), stream))
 
 
 def lynx_kv_dequant(L: Layout, B: int, max_n: int, starts, counts, block_table, k_codes, v_codes, meta: Meta,
                     k_out, v_out, stream=None) -> None:
     """k_out, v_out: BF16 [B][max_n][Hkv][128] (device, written)."""
-    fn = "lynx_kv_dequant"
+    fn, (dev, stream) = "lynx_kv_dequant", _here(stream)
     nb = max(B, 0)
     n = nb * max(max_n, 0) * L.num_kv_heads * HEAD_DIM * 2
     _check(fn, load().lynx_kv_dequant(
-        ctypes.byref(L.c()), B, max_n, _typed(fn, "starts", starts, nb * 4, _I32),
-        _typed(fn, "counts", counts, nb * 4, _I32),
-        _typed(fn, "block_table", block_table, nb * L.max_blocks_per_seq * 4, _I32),
-        _typed(fn, "k_codes", k_codes, L.plane_bytes(128), _U8), _typed(fn, "v_codes", v_codes, L.plane_bytes(128), _U8),
-        ctypes.byref(_typed_meta(fn, L, meta, nb)), _typed(fn, "k_out", k_out, n, _BF16),
-        _typed(fn, "v_out", v_out, n, _BF16), _stream(stream)))
+        _packed(L), B, max_n, _typed(fn, "starts", starts, nb * 4, _I32, dev),
+        _typed(fn, "counts", counts, nb * 4, _I32, dev),
+        _typed(fn, "block_table", block_table, nb * L.max_blocks_per_seq * 4, _I32, dev),
+        _typed(fn, "k_codes", k_codes, L.plane_bytes(128), _U8, dev), _typed(fn, "v_codes", v_codes, L.plane_bytes(128), _U8, dev),
+        _typed_meta(fn, L, meta, nb, dev), _typed(fn, "k_out", k_out, n, _BF16, dev),
+        _typed(fn, "v_out", v_out, n, _BF16, dev), stream))
 
 
 # ----------------------------------------------------------------------------
