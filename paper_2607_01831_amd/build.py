@@ -12,8 +12,8 @@ HERE = Path(__file__).resolve().parent
 CSRC = HERE / "csrc"
 ROOT = HERE.parent
 LIBRARY = HERE / "liblynx.so"
-SOURCES = ["codec.hip", "hier.hip", "attention.hip", "anchor_decode.hip", "anchor_split.hip", "verify.hip", "tree.hip",
-           "append.hip", "spec.hip", "spec_tree.hip", "abi.hip"]
+SOURCES = ["codec.hip", "hier.hip", "attention.hip", "anchor_decode.hip", "anchor_split.hip", "verify.hip",
+           "verify_wide.hip", "tree.hip", "append.hip", "spec.hip", "spec_tree.hip", "abi.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [

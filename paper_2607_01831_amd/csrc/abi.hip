@@ -4,6 +4,7 @@
 #include "../../include/lynx.h"
 #include "lynx_internal.h"
 
+#include <algorithm>
 #include <mutex>
 
 namespace {
@@ -181,8 +182,10 @@ size_t lynx_attn_workspace_bytes(const lynx_layout *L, int32_t B, int32_t Hq,
         max_seq_len < 0)
         return 0;
     const size_t bound = lynx::attention_workspace_bound(g, B, Hq, num_queries, max_seq_len);
+    // (a tree of as many nodes is one of the calls that it serves)
+    const size_t tree = lynx::tree_workspace_bound(g, B, Hq, num_queries, max_seq_len);
     const size_t limit = num_queries == 1 ? lynx::decode_limit_bytes(g, B, Hq, max_seq_len) : 0;
-    return bound > limit ? bound : limit;
+    return std::max(std::max(bound, tree), limit);
 }
 
 int lynx_attn_anchor_decode(const lynx_layout *L, int32_t B, int32_t Hq, int32_t max_seq_len,
@@ -555,11 +558,13 @@ static_assert(LYNX_OPEN_ROWS == lynx::kOpenRows, "header and library disagree");
 
 extern "C" {
 
-int lynx_attn_verify_tree(const lynx_layout *L, int32_t B, int32_t Hq, int32_t n, int32_t max_seq_len,
-                          const int32_t *seq_lens, const int32_t *block_table, const uint8_t *k_codes,
-                          const uint8_t *v_codes, const lynx_meta *meta, const void *q_bf16, const void *k_new,
-                          const void *v_new, const int32_t *parents, void *out_bf16, void *workspace,
-                          size_t workspace_bytes, void *stream) {
+// The context's kernel: wide 1 or 0, or -1 by the rule.  Not in lynx.h: tests
+// reach either kernel at any size.
+int lynx_internal_verify_tree(const lynx_layout *L, int32_t B, int32_t Hq, int32_t n, int32_t max_seq_len,
+                              const int32_t *seq_lens, const int32_t *block_table, const uint8_t *k_codes,
+                              const uint8_t *v_codes, const lynx_meta *meta, const void *q_bf16, const void *k_new,
+                              const void *v_new, const int32_t *parents, void *out_bf16, void *workspace,
+                              size_t workspace_bytes, void *stream, int32_t wide) {
     Geometry g;
     MetaPtrs mp;
     int rc = check_attention_common(L, B, Hq, max_seq_len, seq_lens, block_table, k_codes, v_codes, meta, q_bf16,
@@ -570,15 +575,25 @@ int lynx_attn_verify_tree(const lynx_layout *L, int32_t B, int32_t Hq, int32_t n
     const void *ptrs[] = {k_new, v_new, parents};
     for (const void *p : ptrs)
         if (!p || !aligned16(p)) return LYNX_EINVAL;
-    const lynx::AttnPlan p = lynx::plan_attention(lynx::KvMode::kCodes, g, B, Hq, n, max_seq_len);
-    if (!workspace || !aligned16(workspace) ||
-        workspace_bytes < lynx::attention_workspace_bound(g, B, Hq, n, max_seq_len))
-        return LYNX_EWORKSPACE;
+    const bool is_wide = wide < 0 ? lynx::tree_is_wide(g, B, Hq, n, max_seq_len) : wide != 0;
+    const lynx::AttnPlan p = lynx::plan_attention(is_wide ? lynx::KvMode::kCodesWide : lynx::KvMode::kCodes, g, B, Hq, n,
+                                                  max_seq_len);
+    const size_t need = wide < 0 ? lynx::tree_workspace_bound(g, B, Hq, n, max_seq_len) : p.workspace_bytes();
+    if (!workspace || !aligned16(workspace) || workspace_bytes < need) return LYNX_EWORKSPACE;
     hipError_t e = lynx::launch_verify_tree(
-        g, p, B, Hq, n, max_seq_len, seq_lens, block_table, k_codes, v_codes, mp, static_cast<const uint16_t *>(q_bf16),
-        static_cast<const uint16_t *>(k_new), static_cast<const uint16_t *>(v_new), parents,
-        static_cast<uint16_t *>(out_bf16), workspace, static_cast<hipStream_t>(stream));
+        is_wide, g, p, B, Hq, n, max_seq_len, seq_lens, block_table, k_codes, v_codes, mp,
+        static_cast<const uint16_t *>(q_bf16), static_cast<const uint16_t *>(k_new), static_cast<const uint16_t *>(v_new),
+        parents, static_cast<uint16_t *>(out_bf16), workspace, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? LYNX_OK : LYNX_EHIP;
+}
+
+int lynx_attn_verify_tree(const lynx_layout *L, int32_t B, int32_t Hq, int32_t n, int32_t max_seq_len,
+                          const int32_t *seq_lens, const int32_t *block_table, const uint8_t *k_codes,
+                          const uint8_t *v_codes, const lynx_meta *meta, const void *q_bf16, const void *k_new,
+                          const void *v_new, const int32_t *parents, void *out_bf16, void *workspace,
+                          size_t workspace_bytes, void *stream) {
+    return lynx_internal_verify_tree(L, B, Hq, n, max_seq_len, seq_lens, block_table, k_codes, v_codes, meta, q_bf16,
+                                     k_new, v_new, parents, out_bf16, workspace, workspace_bytes, stream, -1);
 }
 
 size_t lynx_spec_tree_workspace_bytes(int32_t B, int32_t n, int32_t vocab) {

@@ -441,9 +441,11 @@ AttnPlan plan_attention(KvMode mode, const Geometry &g, int B, int Hq, int nq, i
                         size_t most) {
     AttnPlan p{};
     p.rows_total = nq * (Hq / g.Hkv);
-    const int tile = mode == KvMode::kCodes && p.rows_total > 16 ? 32 : 16;  // rows per workgroup
+    // rows per workgroup
+    const int tile = mode == KvMode::kCodesWide ? kWideRows : mode == KvMode::kCodes && p.rows_total > 16 ? 32 : 16;
     const long long chunks = (p.rows_total + tile - 1) / tile;
-    const long long slots = resident_workgroups();
+    // (a wide workgroup is the only one of its CU)
+    const long long slots = mode == KvMode::kCodesWide ? resident_workgroups() / 2 : resident_workgroups();
     const long long units = (long long)B * work_units(max_seq_len);
     const size_t row_bytes = (size_t)g.Hkv * p.rows_total * kPartialBytes;
     // A workgroup per unit of the longest sequence where those of all sequences
@@ -485,6 +487,31 @@ size_t attention_workspace_bound(const Geometry &g, int B, int Hq, int nq, int m
     const size_t by_slots = resident > rows ? resident : rows;
     const size_t by_units = rows * B * (size_t)work_units(max_seq_len);
     return kCounterBytes + ((by_slots < by_units ? by_slots : by_units) + rows * B) * kPartialBytes;
+}
+
+// As above with kWideRows rows per workgroup of the wide kernel (one per CU),
+// for every call that is wide or has room for a smaller one that is.
+size_t tree_workspace_bound(const Geometry &g, int B, int Hq, int n, int max_seq_len) {
+    const size_t narrow = attention_workspace_bound(g, B, Hq, n, max_seq_len);
+    if (3 * n * (long long)(Hq / g.Hkv) < 2 * kWideRows) return narrow;
+    const size_t rows = (size_t)n * Hq;
+    const size_t resident = (size_t)resident_workgroups() / 2 * kWideRows;
+    const size_t by_slots = resident > rows ? resident : rows;
+    const size_t by_units = rows * B * (size_t)work_units(max_seq_len);
+    const size_t wide = kCounterBytes + ((by_slots < by_units ? by_slots : by_units) + rows * B) * kPartialBytes;
+    return wide > narrow ? wide : narrow;
+}
+
+// The wide kernel's workgroup serves kWideRows rows at one price, and a segment
+// of it has a prologue and an epilogue of some 20 us: it pays where the rows
+// fill two thirds of its chunks and a workgroup has 1024 tokens at least.  2 x
+// 64K tokens of 8 kv heads: 192 rows 259 us, wide 200; 128 rows 192 and 199; 320
+// rows 393 and 366; 288 rows 352 and 366; 512 rows 567 and 366.  One sequence, 256
+// rows: 32K tokens (1024 a workgroup) 85 us, wide 79; 16K 50 and 55.
+bool tree_is_wide(const Geometry &g, int B, int Hq, int n, int max_seq_len) {
+    const int rows = n * (Hq / g.Hkv), chunks = (rows + kWideRows - 1) / kWideRows;
+    return 3ll * rows >= 2ll * chunks * kWideRows &&
+           (long long)B * max_seq_len * g.Hkv * chunks >= 1024 * (resident_workgroups() / 2);
 }
 
 // A partial per split of every sequence, splits of 512 tokens, longer (to 2048)
@@ -549,16 +576,16 @@ static VerifyArgs verify_args(const Geometry &g, const AttnPlan &plan, int B, in
     return v;
 }
 
-hipError_t launch_verify_tree(const Geometry &g, const AttnPlan &plan, int B, int Hq, int n, int max_seq_len,
+hipError_t launch_verify_tree(bool wide, const Geometry &g, const AttnPlan &plan, int B, int Hq, int n, int max_seq_len,
                               const int32_t *seq_lens, const int32_t *block_table, const uint8_t *k_codes,
                               const uint8_t *v_codes, MetaPtrs meta, const uint16_t *q, const uint16_t *k_new,
                               const uint16_t *v_new, const int32_t *parents, uint16_t *out, void *workspace,
                               hipStream_t stream) {
     float *ws_o = reinterpret_cast<float *>(reinterpret_cast<char *>(workspace) + kCounterBytes);
     float2 *ws_ml = reinterpret_cast<float2 *>(reinterpret_cast<char *>(workspace) + kCounterBytes + plan.o_bytes);
-    hipError_t e = launch_verify_mfma(verify_args(g, plan, B, Hq, n, max_seq_len, seq_lens, block_table, k_codes,
-                                                  v_codes, meta, q, ws_o, ws_ml),
-                                      stream);
+    const VerifyArgs v = verify_args(g, plan, B, Hq, n, max_seq_len, seq_lens, block_table, k_codes, v_codes, meta, q,
+                                     ws_o, ws_ml);
+    hipError_t e = wide ? launch_verify_wide(v, stream) : launch_verify_mfma(v, stream);
     if (e != hipSuccess) return e;
     TreeArgs a;
     a.geo = g;

@@ -10,7 +10,15 @@ range.  A score is off by at most 2^-21 sum_d |q_d s_d c_d| / sqrt(128) (the
 query in two fp16 parts, 2^-22, and the fp32 sums): with |q s c| <= 64 a dim
 that is below 3.5e-4, and a weight then off by 3.5e-4 of it, the output by 3.5e-4
 range.  The range of V is below 10 here (N(0, 1) values), and of the node's own
-values too: 10 (2^-11 + 3.5e-4) = 8.4e-3."""
+values too: 10 (2^-11 + 3.5e-4) = 8.4e-3.
+The wide kernel rounds V (2^-12 of the segment's largest at most) and K to fp16
+as well: each of a score's 128 terms is off by up to 2^-11 |q k|, independently;
+with an rms of |q k| of 1.6 (two channels of 8) that is 2.3e-4 2^0.5 rms in a
+score, 1.3e-3 at four standard deviations, in the weights of single tokens with
+signs of their own.  An output, a mean of at least some ten such tokens' values of
+either sign, moves by less than a tenth of range 1.3e-3: inside the same bound."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -41,15 +49,33 @@ def inputs_of(c, Hq, n, seed=7):
             random_bf16((c.B, n, c.Hkv, 128), seed + 2))
 
 
-def run(c, q, kn, vn, parents, out=None, ws=None, max_len=None):
+def run(c, q, kn, vn, parents, out=None, ws=None, max_len=None, wide=None):
     B, n, Hq, _ = q.shape
     max_len = max(c.lens) if max_len is None else max_len
     out = torch.full((B, n, Hq, 128), 7.0, dtype=torch.bfloat16, device="cuda") if out is None else out
     ws = lynx.workspace(c.L, B, Hq, n, max_len) if ws is None else ws
-    note(f"verify_tree B={B} n={n} Hq={Hq} Hkv={c.Hkv} bt={c.bt} lens={c.lens[:4]}")
+    note(f"verify_tree B={B} n={n} Hq={Hq} Hkv={c.Hkv} bt={c.bt} lens={c.lens[:4]} wide={wide}")
+    if wide is not None:
+        return run_wide(c, q, kn, vn, parents, out, max_len, wide)
     lynx.lynx_attn_verify_tree(c.L, B, Hq, n, max_len, c.lens_dev(), c.table_dev(), c.pool.k_codes, c.pool.v_codes,
                                c.pool.meta, q.cuda(), kn.cuda(), vn.cuda(),
                                torch.as_tensor(np.asarray(parents, np.int32)).cuda(), out, ws)
+    torch.cuda.synchronize()
+    return out.float().cpu().numpy()
+
+
+def run_wide(c, q, kn, vn, parents, out, max_len, wide):
+    """The same with the context's kernel given."""
+    B, n, Hq, _ = q.shape
+    ws = torch.zeros(64 << 20, dtype=torch.uint8, device="cuda")
+    f = lynx.load().lynx_internal_verify_tree
+    P, I = ctypes.c_void_p, ctypes.c_int32
+    f.argtypes = [P, I, I, I, I, P, P, P, P, P, P, P, P, P, P, P, ctypes.c_size_t, P, I]
+    dev = [c.lens_dev(), c.table_dev(), c.pool.k_codes, c.pool.v_codes, q.cuda(), kn.cuda(), vn.cuda(),
+           torch.as_tensor(np.asarray(parents, np.int32)).cuda(), out, ws]
+    lens, table, kc, vc, qd, kd, vd, pd, od, wd = (x.data_ptr() for x in dev)
+    assert f(ctypes.byref(c.L.c()), B, Hq, n, max_len, lens, table, kc, vc, ctypes.byref(c.pool.meta.c()), qd, kd, vd, pd, od,
+             wd, ws.nbytes, torch.cuda.current_stream().cuda_stream, int(wide)) == 0
     torch.cuda.synchronize()
     return out.float().cpu().numpy()
 
@@ -60,6 +86,7 @@ def want(c, q, kn, vn, parents, lens=None):
                             bits(kn), bits(vn), parents)
 
 
+@pytest.mark.parametrize("wide", [None, True])
 @pytest.mark.parametrize("lens,Hkv,G,n,bt", [
     ([1], 1, 1, 1, None),
     ([0], 2, 4, 5, None),               # no context: the tree alone
@@ -73,12 +100,61 @@ def want(c, q, kn, vn, parents, lens=None):
     ([1200] * 5, 2, 1, 9, 64),
     ([20000], 1, 4, 12, None),          # many partials a row
     ([64] * 70, 1, 2, 3, 16),           # more sequences than lanes
+    ([4100], 1, 8, 64, 16),             # 512 rows
+    ([90, 3000, 0, 129, 520], 1, 5, 60, 48),
 ])
-def test_trees(lens, Hkv, G, n, bt):
+def test_trees(lens, Hkv, G, n, bt, wide):
     c = cache(lens, Hkv, bt)
     x = inputs_of(c, Hkv * G, n)
     parents = random_parents(c.B, n, seed=n)
-    assert_close(run(c, *x, parents), want(c, *x, parents), ATOL, RTOL, "tree")
+    assert_close(run(c, *x, parents, wide=wide), want(c, *x, parents), ATOL, RTOL, "tree")
+
+
+def test_a_wide_call():
+    """A call that the rule gives to the wide kernel, against the other one."""
+    c = cache([131072 + 77], 2, 16)
+    x = inputs_of(c, 8, 64)
+    parents = random_parents(1, 64, seed=9)
+    got, wide, narrow = (run(c, *x, parents, wide=w) for w in (None, True, False))
+    assert np.array_equal(got, wide)
+    assert_close(wide, narrow, ATOL, RTOL * 2, "wide")
+
+
+def wide_inputs(kind):
+    """Caches and queries whose ranges differ by many powers of two."""
+    c = cache([1500, 333], 2, 16)
+    m = c.pool.meta
+    q, kn, vn = inputs_of(c, 8, 30)
+    if kind == "k":      # channel 5: K large where the queries are 0, and 0 where they are large
+        for x in (m.k_scale, m.k_zero):
+            x[:, 0, :, 5] = 0
+            x[:, 1, :, 5] *= 2.0 ** 60
+        q[:, :, :4, 5] *= 2.0 ** 60
+        q[:, :, 4:, 5] = 0
+    if kind == "v":      # V large and small
+        for x in (m.v_scale, m.v_zero):
+            x[:, 0] *= 2.0 ** 90
+            x[:, 1] *= 2.0 ** -90
+    if kind == "groups":  # one group's K a thousand times smaller than the others'
+        for x in (m.k_scale, m.k_zero):
+            x[:, :, 1] *= 2.0 ** -10
+    return c, q, kn, vn
+
+
+@pytest.mark.parametrize("kind", ["k", "v", "groups"])
+@pytest.mark.parametrize("wide", [False, True])
+def test_wide_ranges(kind, wide):
+    c, q, kn, vn = wide_inputs(kind)
+    parents = random_parents(2, 30, seed=4)
+    if kind == "v":  # the context alone: each kv head's values have one size
+        vn[:] = 0
+    got, ref = run(c, q, kn, vn, parents, wide=wide), want(c, q, kn, vn, parents)
+    if kind == "v":
+        got, ref = got.astype(np.float64), ref.copy()
+        for x in (got, ref):
+            x[:, :, :4] *= 2.0 ** -90
+            x[:, :, 4:] *= 2.0 ** 90
+    assert_close(got, ref, ATOL, RTOL, kind)
 
 
 def test_a_chain_is_the_linear_verification():
@@ -147,8 +223,9 @@ def test_lengths_past_the_bound_and_bad_blocks():
     c.table = c.table.clone()
     c.table[1, 3] = c.n_blocks  # of sequence 1 alone
     parents[1, 4] = -2
-    got = run(c, *x, parents)
-    assert np.isfinite(got[0]).all() and np.isnan(got[1, :4]).all() and (got[1, 4] == 0).all()
+    for wide in (None, True):
+        got = run(c, *x, parents, wide=wide)
+        assert np.isfinite(got[0]).all() and np.isnan(got[1, :4]).all() and (got[1, 4] == 0).all()
 
 
 def test_another_stream_a_shared_workspace_and_a_graph():
