@@ -240,7 +240,7 @@ __global__ __launch_bounds__(kThreads) void dequant_kernel(DequantArgs a) {
     constexpr int kStep = 16 / HEADS;        // tokens per pass
     constexpr int kTokens = kStep * PASSES;  // tokens per workgroup, inside one K group
     const int which = RING ? 0 : blockIdx.x & 1, h0 = (RING ? blockIdx.x : blockIdx.x >> 1) * HEADS;
-    const int u = blockIdx.y, b = blockIdx.z;
+    const int u = a.unit0 + blockIdx.y, b = blockIdx.z;
     const int tid = threadIdx.x, m = tid & 15, h = h0 + (tid >> 4) % HEADS, tr = (tid >> 4) / HEADS;
     const int Hkv = a.geo.Hkv;
     int first, end;
@@ -305,13 +305,16 @@ __global__ __launch_bounds__(kThreads) void dequant_kernel(DequantArgs a) {
 }
 
 template <bool RING, int HEADS>
-void launch_dequant_heads(const DequantArgs &a, int B, int rows, hipStream_t stream) {
+void launch_dequant_heads(DequantArgs a, int B, int rows, hipStream_t stream) {
     constexpr int kPasses = 4;  // (8: 139 us for 2 x 64K tokens, 8.9 for 16 x 128; 4: 124 and 4.7)
     constexpr int kTokens = 16 / HEADS * kPasses;
     static_assert(kKGroup % kTokens == 0, "a workgroup stays in one K group");
-    const unsigned units = (unsigned)((rows + 2 * kTokens - 2) / kTokens);
-    hipLaunchKernelGGL((dequant_kernel<RING, HEADS, kPasses>), dim3((RING ? 1 : 2) * a.geo.Hkv / HEADS, units, B),
-                       dim3(kThreads), 0, stream, a);
+    constexpr int kMostUnits = 65535;  // of a grid; more rows (524K at 8 heads) take a launch more
+    const int units = (rows + 2 * kTokens - 2) / kTokens;
+    for (a.unit0 = 0; a.unit0 < units; a.unit0 += kMostUnits)
+        hipLaunchKernelGGL((dequant_kernel<RING, HEADS, kPasses>),
+                           dim3((RING ? 1 : 2) * a.geo.Hkv / HEADS, min(kMostUnits, units - a.unit0), B),
+                           dim3(kThreads), 0, stream, a);
 }
 template <bool RING>
 hipError_t launch_dequant_any(const DequantArgs &a, int B, int rows, hipStream_t stream) {

@@ -280,6 +280,7 @@ struct AppendArgs {
 struct DequantArgs {
     Geometry geo;
     int max_n;                // rows of the output per sequence
+    int unit0;                // the launch's first unit of rows (set by the launcher)
     int capacity;
     int bt_shift;
     const int32_t *starts;    // [B]; append_begin: the lengths

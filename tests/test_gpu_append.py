@@ -258,6 +258,34 @@ def test_read_back(lens, Hkv, bt):
                 assert (o[b, n:] == 7).all()
 
 
+@pytest.mark.parametrize("Hkv", [4, 6, 8, 12, 16])
+def test_read_back_many_heads(Hkv):
+    test_read_back([300, 77], Hkv, 16)
+
+
+def test_read_back_of_more_rows_than_a_grid_holds():
+    # 8 heads: workgroups of 8 rows, 65535 of them a launch
+    T, Hkv, first = 530_000, 8, 3
+    L = lynx.Layout(num_kv_heads=Hkv, block_tokens=T, max_blocks_per_seq=1, num_blocks=1, max_tokens=T)
+    g = torch.Generator("cuda").manual_seed(1)
+    codes = [torch.randint(0, 256, (Hkv, T, 128), dtype=torch.uint8, device="cuda", generator=g) for _ in range(2)]
+    meta = lynx.Meta.empty(L, 1)
+    for x in (meta.k_scale, meta.k_zero, meta.v_scale, meta.v_zero):
+        x.copy_(torch.randn(x.shape, device="cuda", generator=g))
+    out = [torch.full((T - first, Hkv, 128), 7.0, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+    ints = lambda x: torch.tensor([x], dtype=torch.int32).cuda()  # noqa: E731
+    note(f"dequant {T - first} rows")
+    lynx.lynx_kv_dequant(L, 1, T - first, ints(first), ints(T - first), ints(0), *codes, meta, *out)
+    torch.cuda.synchronize()
+    for at in (first, 2 ** 18, 65535 * 8 - 500, T - 1000):
+        t = torch.arange(at, at + 1000, device="cuda")
+        ks, kz = (x.view(Hkv, -1, 128)[:, t // 128].double() for x in (meta.k_scale, meta.k_zero))
+        vs, vz = (x.view(Hkv, T, 1)[:, t].double() for x in (meta.v_scale, meta.v_zero))
+        for o, c, sc, z in ((out[0], codes[0], ks, kz), (out[1], codes[1], vs, vz)):
+            want = (c[:, t].double() * sc + z).transpose(0, 1)
+            assert_close(o[t - first].float().cpu().numpy(), want.cpu().numpy(), 0.0, 2.0 ** -8 + 2.0 ** -23, "values")
+
+
 def test_read_back_out_of_range():
     kv = random_kv(200, 2, seed=1)
     c = build_cache([kv[0]] * 5, [kv[1]] * 5, 2, bt=16)
