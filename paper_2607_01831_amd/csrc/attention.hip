@@ -607,7 +607,16 @@ hipError_t launch_verify_tree(bool wide, const Geometry &g, const AttnPlan &plan
     a.ws_o = ws_o;
     a.ws_ml = ws_ml;
     a.out = out;
-    return launch_tree_combine(a, stream);
+    // Rows of more than 4 partials go four to a workgroup, whose groups of threads
+    // share them, while all those workgroups are on the device at once; else 16,
+    // which read the nodes' values once.  Per call, us, by four and by 16 rows: one
+    // sequence of 4K, 32 rows: 17.6 and 18.8; of 64K, 32 rows: 39.5 and 50.1; of
+    // 16K, 256 rows (512 workgroups): 46.0 and 46.7; 2 of 4K, 256 rows (1024): 35.4
+    // and 32.9; 16 of 4K, 100 rows (3200): 107 and 92; 48 of 1K, 256 rows: 254 and
+    // 145; 4 partials, 8 of 2K, 32 rows (512): 20.2 and 19.2.
+    const int each = plan.direct ? plan.direct : std::min(plan.max_live, plan.workers / B + 1);
+    const long long fours = (long long)((plan.rows_total + 3) / 4) * g.Hkv * B;
+    return launch_tree_combine(a, each > 4 && fours <= resident_workgroups() ? 4 : 16, stream);
 }
 
 hipError_t launch_attention(KvMode mode, const Geometry &g, const AttnPlan &plan, int B, int Hq,

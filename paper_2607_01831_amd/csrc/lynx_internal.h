@@ -248,7 +248,8 @@ struct TreeArgs {
     uint16_t *out;                 // BF16 [B][n][Hq][128]
 };
 
-hipError_t launch_tree_combine(const TreeArgs &args, hipStream_t stream);
+// rows: those of a workgroup, 4 or 16.
+hipError_t launch_tree_combine(const TreeArgs &args, int rows, hipStream_t stream);
 // The tree's rows over the context (plan_attention of KvMode::kCodes, or
 // kCodesWide, with n queries), then the merge.
 hipError_t launch_verify_tree(bool wide, const Geometry &g, const AttnPlan &plan, int B, int Hq, int n, int max_seq_len,

@@ -282,9 +282,8 @@ void launch_rows(const TreeArgs &a, hipStream_t stream) {
 
 }  // namespace
 
-hipError_t launch_tree_combine(const TreeArgs &a, hipStream_t stream) {
-    const int each = a.direct ? a.direct : a.B == 1 ? a.max_live : a.max_live < a.workers / a.B + 1 ? a.max_live : a.workers / a.B + 1;
-    if (each > 8)
+hipError_t launch_tree_combine(const TreeArgs &a, int rows, hipStream_t stream) {
+    if (rows == 4)
         launch_rows<4>(a, stream);
     else
         launch_rows<16>(a, stream);
