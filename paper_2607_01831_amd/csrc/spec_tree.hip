@@ -314,7 +314,7 @@ __global__ __launch_bounds__(kThreads) void tree_rows_kernel(TreeAcceptArgs a) {
     uint64_t *words = a.words + r * a.chunks;
     const float *x = a.scores + r * a.vocab;
     __shared__ uint64_t s_wave[kWaves], s_left;
-    __shared__ int s_at, s_last;
+    __shared__ int s_at, s_last, s_chunk;
     __shared__ float s_x[SAMPLE ? (PER + 1) * kThreads : 1];
     float v[PER];
     load_chunk(x, lo, a.vocab, vec4, v);
@@ -333,12 +333,12 @@ __global__ __launch_bounds__(kThreads) void tree_rows_kernel(TreeAcceptArgs a) {
             look(words, a.chunks, first);
             const int at = drawn_chunk(words, a.chunks, first, a.uniforms[r], left);
             if (lane == 0) {
-                s_last = at;
+                s_chunk = at;
                 s_left = left;
             }
         }
         __syncthreads();
-        choice = s_last;
+        choice = s_chunk;
         if (choice >= 0) {
             const int at = choice * PER * kThreads;
             load_chunk(x, at, a.vocab, vec4, v);
@@ -416,9 +416,10 @@ __global__ __launch_bounds__(kThreads) void tree_path_kernel(TreeAcceptArgs a) {
         const uint64_t word = chunk_word<SAMPLE>(v, lo, vec4, s_wave);
         if (tid == 0) agent_store(words + c, word);
         const float uniform = SAMPLE ? a.uniforms[r0 + row] : 0.0f;
+        bool in = false;  // (of the first wavefront)
         if (w == 0) {
             uint64_t left = 0, first = 0;
-            const bool in = wait([&] { return look(words, a.chunks, first); });
+            in = wait([&] { return look(words, a.chunks, first); });
             int draw = -1;
             if (in) {
                 if (SAMPLE)
@@ -429,41 +430,41 @@ __global__ __launch_bounds__(kThreads) void tree_path_kernel(TreeAcceptArgs a) {
             if (lane == 0) {
                 s_draw = in ? draw : kLate;
                 s_left = left;
-                s_row = in ? 0 : kLate;
             }
         }
         if (SAMPLE) {
             __syncthreads();
             const int draw = s_draw;
-            if (draw == kLate) break;
+            if (draw == kLate) {
+                row = kLate;
+                break;
+            }
             if (draw == c) {  // the draw falls into this chunk: the others wait for its entry
                 const int entry = drawn_entry(v, lo, vec4, s_left, s_wave, s_x, &s_at);
                 if (tid == 0) agent_store(&state[row].choice, entry + 2);
             }
             if (w == 0) {
                 int got = 1;  // no weight at all: -1
-                const bool in = draw < 0 || wait([&] { return (got = agent_load(&state[row].choice)) != 0; });
+                in = draw < 0 || wait([&] { return (got = agent_load(&state[row].choice)) != 0; });
                 choice = got - 2;
-                if (!in && lane == 0) s_row = kLate;
-                if (!in) choice = -1;
             }
         }
         if (w == 0) {
-            const int j = s_row == kLate ? -1 : tree.next(at, choice);
+            const int j = in ? tree.next(at, choice) : -1;
             if (j >= 0) {
                 at = j;
                 if (lane == kept) mine = j;
                 ++kept;
                 done |= 1ull << j;
             }
-            if (lane == 0 && s_row != kLate) s_row = j >= 0 ? j + 1 : kEnd;
+            if (lane == 0) s_row = !in ? kLate : j >= 0 ? j + 1 : kEnd;
         }
         __syncthreads();
         row = s_row;
         __syncthreads();
         if (row < 0) break;
     }
-    const bool late = s_row == kLate;
+    const bool late = row == kLate;
     if (late) {
         // the others may never come while this workgroup is here: its chunk of
         // every other row, and away
@@ -499,6 +500,7 @@ __global__ __launch_bounds__(kThreads) void tree_path_kernel(TreeAcceptArgs a) {
             if (SAMPLE && got >= 0) {
                 load_chunk(a.scores + (r0 + row) * V, got * PER * kThreads, V, vec4, v);
                 choice = drawn_entry(v, got * PER * kThreads, vec4, left, s_wave, s_x, &s_at);
+                __syncthreads();  // every wavefront has it
             }
             const int j = tree.next(at, choice);  // every wavefront walks
             if (j >= 0) {
