@@ -59,7 +59,7 @@ constexpr int kRawMeta = 2 * kRawPlane;             // V scale[32] | V zero[32]
 constexpr int kRawBytes = kRawMeta + 2 * kTile * 4;
 constexpr int kFragBytes = 8 * 1024;                // a tile's 8 fragments of K, or of V
 constexpr int kFragsV = 3;                          // V's buffers; K's are two
-constexpr int kDepth = 4;                      // tiles whose copies are in flight or not converted yet
+constexpr int kDepth = 4;                           // tiles whose copies are in flight or not converted yet
 constexpr float kSlack = 8.0f;                      // log2 units that the reference may lag behind
 
 template <int LAYOUT>
@@ -373,11 +373,11 @@ __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<
 #pragma unroll
             for (int r = 0; r < 2; ++r) s[rt][r] = ahead[rt][r];
         // tile j + 3 is in once only the later ones' operations are in flight
-        switch (min(kDepth, n_tiles - 1 - j) - 3) {
-        case 2: wait_vmcnt<2 * kOps>(); break;
-        case 1: wait_vmcnt<kOps>(); break;
-        default: wait_vmcnt<0>(); break;
-        }
+        static_assert(kDepth == 4, "one tile's may be");
+        if (j + kDepth < n_tiles)
+            wait_vmcnt<kOps>();
+        else
+            wait_vmcnt<0>();
         __syncthreads();
     }
 
