@@ -241,37 +241,39 @@ __device__ __forceinline__ int drawn_chunk(const uint64_t *words, int chunks, ui
     }
 }
 
-// The entry of a chunk (held as load_chunk gives it) at which the chunk's weights
-// pass `left`; by the workgroup, the same in every thread.  The chunk goes
-// through LDS, so that a thread has PER entries in order and one scan does (16
+// A chunk (held as load_chunk gives it) laid out for its draw: through LDS, so
+// that thread tid has entries PER tid .. + PER - 1 and one scan does (16
 // sequences, 50257 entries, 6 kept, along the path: 38 us, with a scan for every
-// 256 entries 62 us).
+// 256 entries 62 us).  The weights before the thread's entries, and theirs.
 template <int PER>
-__device__ __forceinline__ int drawn_entry(const float (&x)[PER], int lo, bool vec4, uint64_t left, uint64_t *s_wave,
-                                           float *s_x, int *s_at) {
+__device__ __forceinline__ int entry_slot(int e) { return e + e / PER; }  // a thread's entries start in another bank
+template <int PER>
+__device__ __forceinline__ uint64_t lay_out(const float (&x)[PER], bool vec4, uint64_t *s_wave, float *s_x, uint64_t &sum) {
     const int tid = threadIdx.x;
-    auto slot = [](int e) { return e + e / PER; };  // a thread's entries start in another bank
 #pragma unroll
     for (int j = 0; j < PER; ++j)
-        s_x[slot(vec4 ? 4 * kThreads * (j / 4) + 4 * tid + j % 4 : kThreads * j + tid)] = x[j];
-    if (tid == 0) *s_at = -1;
+        s_x[entry_slot<PER>(vec4 ? 4 * kThreads * (j / 4) + 4 * tid + j % 4 : kThreads * j + tid)] = x[j];
     __syncthreads();
-    uint64_t w[PER], sum = 0, all;
+    uint32_t upper = 0, lower = 0;
 #pragma unroll
-    for (int j = 0; j < PER; ++j) sum += w[j] = weight(s_x[slot(PER * tid + j)]);
-    const uint64_t before = block_scan(sum, s_wave, all);
-    if (left >= before && left - before < sum) {
-        uint64_t upto = before;
-        int at = -1;
+    for (int j = 0; j < PER; ++j) weight_parts(s_x[entry_slot<PER>(PER * tid + j)], upper, lower);
+    sum = ((uint64_t)upper << 20) + lower;
+    uint64_t all;
+    return block_scan(sum, s_wave, all);
+}
+// The entry at which the chunk's weights pass `left`, in the thread that has it;
+// -1 in the others.
+template <int PER>
+__device__ __forceinline__ int drawn_entry(const float *s_x, int lo, uint64_t left, uint64_t before, uint64_t sum) {
+    if (left < before || left - before >= sum) return -1;
+    int at = PER - 1;
+    uint64_t upto = before + sum;
 #pragma unroll
-        for (int j = 0; j < PER; ++j) {
-            upto += w[j];
-            if (at < 0 && upto > left) at = lo + PER * tid + j;
-        }
-        *s_at = at;
+    for (int j = PER - 1; j > 0; --j) {
+        upto -= weight(s_x[entry_slot<PER>(PER * threadIdx.x + j)]);  // the weights of the entries before j
+        if (upto > left) at = j - 1;
     }
-    __syncthreads();
-    return *s_at;
+    return lo + PER * threadIdx.x + at;
 }
 
 // The tree in a wavefront, a node in each lane.
@@ -342,7 +344,12 @@ __global__ __launch_bounds__(kThreads) void tree_rows_kernel(TreeAcceptArgs a) {
         if (choice >= 0) {
             const int at = choice * PER * kThreads;
             load_chunk(x, at, a.vocab, vec4, v);
-            choice = drawn_entry(v, at, vec4, s_left, s_wave, s_x, &s_at);
+            uint64_t sum;
+            const uint64_t before = lay_out(v, vec4, s_wave, s_x, sum);
+            const int entry = drawn_entry<PER>(s_x, at, s_left, before, sum);
+            if (entry >= 0) s_at = entry;
+            __syncthreads();
+            choice = s_at;
         }
     } else {
         choice = 0;
@@ -416,7 +423,9 @@ __global__ __launch_bounds__(kThreads) void tree_path_kernel(TreeAcceptArgs a) {
         const uint64_t word = chunk_word<SAMPLE>(v, lo, vec4, s_wave);
         if (tid == 0) agent_store(words + c, word);
         const float uniform = SAMPLE ? a.uniforms[r0 + row] : 0.0f;
-        bool in = false;  // (of the first wavefront)
+        uint64_t before = 0, sum = 0;
+        if (SAMPLE) before = lay_out(v, vec4, s_wave, s_x, sum);  // in case the draw falls here, while the words come in
+        bool in = false;                                         // (of the first wavefront)
         if (w == 0) {
             uint64_t left = 0, first = 0;
             in = wait([&] { return look(words, a.chunks, first); });
@@ -440,8 +449,8 @@ __global__ __launch_bounds__(kThreads) void tree_path_kernel(TreeAcceptArgs a) {
                 break;
             }
             if (draw == c) {  // the draw falls into this chunk: the others wait for its entry
-                const int entry = drawn_entry(v, lo, vec4, s_left, s_wave, s_x, &s_at);
-                if (tid == 0) agent_store(&state[row].choice, entry + 2);
+                const int entry = drawn_entry<PER>(s_x, lo, s_left, before, sum);
+                if (entry >= 0) agent_store(&state[row].choice, entry + 2);
             }
             if (w == 0) {
                 int got = 1;  // no weight at all: -1
@@ -499,7 +508,12 @@ __global__ __launch_bounds__(kThreads) void tree_path_kernel(TreeAcceptArgs a) {
             choice = got;
             if (SAMPLE && got >= 0) {
                 load_chunk(a.scores + (r0 + row) * V, got * PER * kThreads, V, vec4, v);
-                choice = drawn_entry(v, got * PER * kThreads, vec4, left, s_wave, s_x, &s_at);
+                uint64_t sum;
+                const uint64_t before = lay_out(v, vec4, s_wave, s_x, sum);
+                const int entry = drawn_entry<PER>(s_x, got * PER * kThreads, left, before, sum);
+                if (entry >= 0) s_at = entry;
+                __syncthreads();
+                choice = s_at;
                 __syncthreads();  // every wavefront has it
             }
             const int j = tree.next(at, choice);  // every wavefront walks
