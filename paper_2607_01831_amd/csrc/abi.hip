@@ -558,8 +558,8 @@ static_assert(LYNX_OPEN_ROWS == lynx::kOpenRows, "header and library disagree");
 
 extern "C" {
 
-// The context's kernel: wide 1 or 0, or -1 by the rule.  Not in lynx.h: tests
-// reach either kernel at any size.
+// The context's kernel: wide 0, 1 or 2 (half the rows per workgroup), or -1 by the
+// rule.  Not in lynx.h: tests reach each of them at any size.
 int lynx_internal_verify_tree(const lynx_layout *L, int32_t B, int32_t Hq, int32_t n, int32_t max_seq_len,
                               const int32_t *seq_lens, const int32_t *block_table, const uint8_t *k_codes,
                               const uint8_t *v_codes, const lynx_meta *meta, const void *q_bf16, const void *k_new,
@@ -575,13 +575,16 @@ int lynx_internal_verify_tree(const lynx_layout *L, int32_t B, int32_t Hq, int32
     const void *ptrs[] = {k_new, v_new, parents};
     for (const void *p : ptrs)
         if (!p || !aligned16(p)) return LYNX_EINVAL;
-    const bool is_wide = wide < 0 ? lynx::tree_is_wide(g, B, Hq, n, max_seq_len) : wide != 0;
-    const lynx::AttnPlan p = lynx::plan_attention(is_wide ? lynx::KvMode::kCodesWide : lynx::KvMode::kCodes, g, B, Hq, n,
-                                                  max_seq_len);
-    const size_t need = wide < 0 ? lynx::tree_workspace_bound(g, B, Hq, n, max_seq_len) : p.workspace_bytes();
+    const lynx::KvMode mode = wide < 0    ? lynx::tree_mode(g, B, Hq, n, max_seq_len)
+                              : wide == 0 ? lynx::KvMode::kCodes
+                              : wide == 1 ? lynx::KvMode::kCodesWide
+                                          : lynx::KvMode::kCodesHalfWide;
+    const lynx::AttnPlan p = lynx::plan_attention(mode, g, B, Hq, n, max_seq_len);
+    const size_t bound = wide < 0 ? lynx::tree_workspace_bound(g, B, Hq, n, max_seq_len) : 0;
+    const size_t need = std::max(bound, p.workspace_bytes());
     if (!workspace || !aligned16(workspace) || workspace_bytes < need) return LYNX_EWORKSPACE;
     hipError_t e = lynx::launch_verify_tree(
-        is_wide, g, p, B, Hq, n, max_seq_len, seq_lens, block_table, k_codes, v_codes, mp,
+        mode, g, p, B, Hq, n, max_seq_len, seq_lens, block_table, k_codes, v_codes, mp,
         static_cast<const uint16_t *>(q_bf16), static_cast<const uint16_t *>(k_new), static_cast<const uint16_t *>(v_new),
         parents, static_cast<uint16_t *>(out_bf16), workspace, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? LYNX_OK : LYNX_EHIP;

@@ -431,6 +431,11 @@ long long work_units(int T) { return T > 0 ? ((long long)T + kWorkUnit * kKGroup
 
 constexpr size_t kPartialBytes = kHeadDim * sizeof(float) + sizeof(float2);
 
+// Query rows a kv head up to which a tree stays with verify.hip's kernel.
+constexpr int kNarrowRows = 64;
+// Rows per workgroup of the wide kernel.
+int wide_rows(KvMode mode) { return mode == KvMode::kCodesHalfWide ? kWideRows / 2 : kWideRows; }
+
 }  // namespace
 
 // One round of workgroups, whatever the batch: as many workers per (kv head,
@@ -442,10 +447,11 @@ AttnPlan plan_attention(KvMode mode, const Geometry &g, int B, int Hq, int nq, i
     AttnPlan p{};
     p.rows_total = nq * (Hq / g.Hkv);
     // rows per workgroup
-    const int tile = mode == KvMode::kCodesWide ? kWideRows : mode == KvMode::kCodes && p.rows_total > 16 ? 32 : 16;
+    const bool wide = mode == KvMode::kCodesWide || mode == KvMode::kCodesHalfWide;
+    const int tile = wide ? wide_rows(mode) : mode == KvMode::kCodes && p.rows_total > 16 ? 32 : 16;
     const long long chunks = (p.rows_total + tile - 1) / tile;
     // (a wide workgroup is the only one of its CU)
-    const long long slots = mode == KvMode::kCodesWide ? resident_workgroups() / 2 : resident_workgroups();
+    const long long slots = wide ? resident_workgroups() / 2 : resident_workgroups();
     const long long units = (long long)B * work_units(max_seq_len);
     const size_t row_bytes = (size_t)g.Hkv * p.rows_total * kPartialBytes;
     // A workgroup per unit of the longest sequence where those of all sequences
@@ -489,29 +495,39 @@ size_t attention_workspace_bound(const Geometry &g, int B, int Hq, int nq, int m
     return kCounterBytes + ((by_slots < by_units ? by_slots : by_units) + rows * B) * kPartialBytes;
 }
 
-// As above with kWideRows rows per workgroup of the wide kernel (one per CU),
-// for every call that is wide or has room for a smaller one that is.
+// As above with the rows per workgroup of the wide kernel (one per CU), for
+// every call that may be wide (tree_mode: half as wide from 65 rows, wide from 129)
+// or has room for a smaller one that is.
 size_t tree_workspace_bound(const Geometry &g, int B, int Hq, int n, int max_seq_len) {
     const size_t narrow = attention_workspace_bound(g, B, Hq, n, max_seq_len);
-    if (3 * n * (long long)(Hq / g.Hkv) < 2 * kWideRows) return narrow;
+    const int rows_kv = n * (Hq / g.Hkv);
+    if (rows_kv <= kNarrowRows) return narrow;
     const size_t rows = (size_t)n * Hq;
-    const size_t resident = (size_t)resident_workgroups() / 2 * kWideRows;
+    const size_t resident = (size_t)resident_workgroups() / 2 * (rows_kv > kWideRows / 2 ? kWideRows : kWideRows / 2);
     const size_t by_slots = resident > rows ? resident : rows;
     const size_t by_units = rows * B * (size_t)work_units(max_seq_len);
     const size_t wide = kCounterBytes + ((by_slots < by_units ? by_slots : by_units) + rows * B) * kPartialBytes;
     return wide > narrow ? wide : narrow;
 }
 
-// The wide kernel's workgroup serves kWideRows rows at one price, and a segment
-// of it has a prologue and an epilogue of some 20 us: it pays where the rows
-// fill two thirds of its chunks and a workgroup has 1024 tokens at least.  2 x
-// 64K tokens of 8 kv heads: 192 rows 259 us, wide 200; 128 rows 192 and 199; 320
-// rows 393 and 366; 288 rows 352 and 366; 512 rows 567 and 366.  One sequence, 256
-// rows: 32K tokens (1024 a workgroup) 85 us, wide 79; 16K 50 and 55.
-bool tree_is_wide(const Geometry &g, int B, int Hq, int n, int max_seq_len) {
-    const int rows = n * (Hq / g.Hkv), chunks = (rows + kWideRows - 1) / kWideRows;
-    return 3ll * rows >= 2ll * chunks * kWideRows &&
-           (long long)B * max_seq_len * g.Hkv * chunks >= 1024 * (resident_workgroups() / 2);
+// The kernel of least estimated time.  verify.hip's serves 32 rows a workgroup, a
+// wide one kWideRows or half of them, whether they are there or not, and a
+// segment of it costs more to begin and to join; per token of a compute unit's
+// share and chunk of rows they take some 10.3, 43.7 and 27.2 ns.  Measured, us, 2
+// sequences of 64K (4096 tokens a unit) of 8 kv heads, narrow, wide and half: 80
+// rows 144, 198, 135; 128 rows 181, 202, 139; 160 rows 227, 204, 240; 256 rows 321,
+// 210, 244; of 16K (1024): 128 rows 53, 68, 55; 192 rows 74, 73, 78; 256 rows 84, 75,
+// 78; of 8K: 128 rows 36, 45, 40; 256 rows 51, 57, 54; 512 rows 84, 73, 78.  16 paged
+// sequences of 1K-8K: 100 rows 136, 168, 123; 256 rows 248, 189, 222.
+KvMode tree_mode(const Geometry &g, int B, int Hq, int n, int max_seq_len) {
+    const int rows = n * (Hq / g.Hkv);
+    if (rows <= kNarrowRows) return KvMode::kCodes;  // (two chunks of 32 cost less than one of either)
+    auto chunks = [&](int each) { return (rows + each - 1) / each; };
+    const double tokens = (double)B * max_seq_len * g.Hkv / (resident_workgroups() / 2);
+    const double narrow = 10.3 * tokens * chunks(32);
+    const double wide = 43.7 * tokens * chunks(kWideRows) + 20000;
+    const double half = 27.2 * tokens * chunks(kWideRows / 2) + 15000;
+    return narrow <= std::min(wide, half) ? KvMode::kCodes : half <= wide ? KvMode::kCodesHalfWide : KvMode::kCodesWide;
 }
 
 // A partial per split of every sequence, splits of 512 tokens, longer (to 2048)
@@ -576,7 +592,7 @@ static VerifyArgs verify_args(const Geometry &g, const AttnPlan &plan, int B, in
     return v;
 }
 
-hipError_t launch_verify_tree(bool wide, const Geometry &g, const AttnPlan &plan, int B, int Hq, int n, int max_seq_len,
+hipError_t launch_verify_tree(KvMode mode, const Geometry &g, const AttnPlan &plan, int B, int Hq, int n, int max_seq_len,
                               const int32_t *seq_lens, const int32_t *block_table, const uint8_t *k_codes,
                               const uint8_t *v_codes, MetaPtrs meta, const uint16_t *q, const uint16_t *k_new,
                               const uint16_t *v_new, const int32_t *parents, uint16_t *out, void *workspace,
@@ -585,7 +601,7 @@ hipError_t launch_verify_tree(bool wide, const Geometry &g, const AttnPlan &plan
     float2 *ws_ml = reinterpret_cast<float2 *>(reinterpret_cast<char *>(workspace) + kCounterBytes + plan.o_bytes);
     const VerifyArgs v = verify_args(g, plan, B, Hq, n, max_seq_len, seq_lens, block_table, k_codes, v_codes, meta, q,
                                      ws_o, ws_ml);
-    hipError_t e = wide ? launch_verify_wide(v, stream) : launch_verify_mfma(v, stream);
+    hipError_t e = mode == KvMode::kCodes ? launch_verify_mfma(v, stream) : launch_verify_wide(v, wide_rows(mode), stream);
     if (e != hipSuccess) return e;
     TreeArgs a;
     a.geo = g;

@@ -103,7 +103,7 @@ hipError_t launch_deserialize_residual(const Geometry &g, int b, int t0, int n,
 constexpr size_t kCounterBytes = 262144;
 constexpr int kCounterStride = 64;  // uint32 slots between counters
 constexpr int kCounters = (int)(kCounterBytes / (kCounterStride * sizeof(unsigned)));
-enum class KvMode : int { kAnchor = 0, kCodes = 1, kAnchorSplit = 2, kCodesWide = 3 };
+enum class KvMode : int { kAnchor = 0, kCodes = 1, kAnchorSplit = 2, kCodesWide = 3, kCodesHalfWide = 4 };
 
 // 128-token groups per unit of the attention kernels' work list (work_list.h):
 // one per wavefront of a workgroup.
@@ -173,9 +173,10 @@ struct VerifyArgs {
 };
 
 hipError_t launch_verify_mfma(const VerifyArgs &args, hipStream_t stream);
-// The same for many rows a kv head (verify_wide.hip), kWideRows per workgroup.
+// The same for many rows a kv head (verify_wide.hip), `rows` per workgroup:
+// kWideRows or half of them.
 constexpr int kWideRows = 256;
-hipError_t launch_verify_wide(const VerifyArgs &args, hipStream_t stream);
+hipError_t launch_verify_wide(const VerifyArgs &args, int rows, hipStream_t stream);
 
 // Arguments of the anchor decode over split-width anchors (anchor_split.hip):
 // one query per sequence over A-bit anchor planes (rows of 16 A bytes).
@@ -217,7 +218,7 @@ size_t attention_workspace_bound(const Geometry &g, int B, int Hq, int nq, int m
 size_t tree_workspace_bound(const Geometry &g, int B, int Hq, int n, int max_seq_len);
 // The kernel of a tree's context part: more rows a kv head than verify.hip's
 // two row tiles serve at less cost.
-bool tree_is_wide(const Geometry &g, int B, int Hq, int n, int max_seq_len);
+KvMode tree_mode(const Geometry &g, int B, int Hq, int n, int max_seq_len);
 // Bytes that lynx_attn_workspace_bytes reports at least for a decode, and that
 // lynx_attn_anchor_decode_noalloc compares with its scratch.
 size_t decode_limit_bytes(const Geometry &g, int B, int Hq, int max_seq_len);
@@ -252,7 +253,7 @@ struct TreeArgs {
 hipError_t launch_tree_combine(const TreeArgs &args, int rows, hipStream_t stream);
 // The tree's rows over the context (plan_attention of KvMode::kCodes, or
 // kCodesWide, with n queries), then the merge.
-hipError_t launch_verify_tree(bool wide, const Geometry &g, const AttnPlan &plan, int B, int Hq, int n, int max_seq_len,
+hipError_t launch_verify_tree(KvMode mode, const Geometry &g, const AttnPlan &plan, int B, int Hq, int n, int max_seq_len,
                               const int32_t *seq_lens, const int32_t *block_table, const uint8_t *k_codes,
                               const uint8_t *v_codes, MetaPtrs meta, const uint16_t *q, const uint16_t *k_new,
                               const uint16_t *v_new, const int32_t *parents, uint16_t *out, void *workspace,

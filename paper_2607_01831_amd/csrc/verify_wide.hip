@@ -4,11 +4,11 @@
 // What it computes is verify.hip's: the partial (max, sum, output) of every row
 // over a segment of the context.  There a wavefront folds the K scales into its
 // own rows' queries, group by group, and unpacks K and V for itself, which costs
-// as many vector instructions per (row, token) as the softmax does.  With 200 rows
+// as many vector instructions per (row, token) as the softmax does.  With 100 rows
 // and more the keys are the smaller side: here the workgroup's 8 wavefronts share
 // the tokens and split the rows, 32 each, so that a tile's K and V are
-// reconstructed once for 256 rows, as fp16 in the matrix cores' operand order in
-// LDS, and the queries are converted once.
+// reconstructed once for 256 rows (or 128), as fp16 in the matrix cores' operand
+// order in LDS, and the queries are converted once.
 //
 // Operands:
 //  * K' = (zero + code scale) 2^-e_d, e_d the exponent of the largest |K| of
@@ -24,17 +24,22 @@
 //    are the weights p <= 2^8 against a reference that follows the row's maximum
 //    once it is 2^8 behind; l is summed in fp32.
 //
-// A tile of 32 tokens costs a wavefront 32 MFMAs for its 32 rows.  Iteration j:
-// copies of tile j + kDepth into LDS (asynchronous), the scores of tile j + 1, the
-// weights of tile j and their products with the values, the conversion of tile
-// j + 2, in one stretch without branches, so that matrix and vector instructions
-// take turns; one barrier.  2 x 64K tokens, 8 kv heads, 512 rows: 361 us with the
-// merge (verify.hip's kernel 560), 32% of the matrix cores' cycles and 45% of the
-// vector ones'; the rest are waits for LDS, whose reads (16 KB per wavefront and
-// tile) come in bursts behind the barrier.  Four wavefronts of 32 rows twice on a
-// CU took 470 us, four of 64 rows 627 (accumulators move through the other half
-// of the register file), two orders of the stretches for the two wavefronts of a
-// SIMD 444.
+// A step is a tile of 32 tokens for 256 rows, or, for half the rows, two tiles
+// with a wavefront's two partners each on one (TS 2; they join at the end).  A
+// tile costs a wavefront 34 MFMAs for its 32 rows (two of them sum the weights,
+// as a column of ones behind the values).  Iteration j: copies of step j + 4 into
+// LDS (asynchronous), the scores of step j + 1 in turns with the weights of step
+// j, the products with the values in turns with the conversion of step j + 2; one
+// barrier.  2 x 64K tokens, 8 kv heads, with the merge: 512 rows 341 us (verify.hip's
+// kernel 560), 128 rows 139 (181).  What bounds it: instructions.  A SIMD has two
+// wavefronts; behind an MFMA's 16 cycles two vector instructions are free and each
+// further one takes 5, and a wavefront's tile has 34 MFMAs and some 135 others,
+// 2000 of the 3200 cycles that it takes; the rest are the barrier and the waits
+// around it.  Without the conversion it would take 33 us less of 200 (256 rows),
+// without the copies 23, without the scores' products 30.  Tried: fragments and
+// codes read a step ahead of the barrier (347 and 170 us: registers), four
+// wavefronts of 32 rows twice on a CU (470), four of 64 rows (627), 128 rows by 16
+// a wavefront (152), two orders of the stretches for the wavefronts of a SIMD (444).
 #include "f16_ops.h"
 #include "lane_ops.h"
 #include "lynx_internal.h"
@@ -50,8 +55,7 @@ typedef _Float16 h2 __attribute__((ext_vector_type(2)));
 
 constexpr int kWaves = 8;
 constexpr int kThreads = 64 * kWaves;
-constexpr int kRows = kWideRows;
-static_assert(kRows == 32 * kWaves, "two row tiles per wavefront");
+static_assert(kWideRows == 32 * kWaves, "two row tiles per wavefront");
 constexpr int kTile = 32;  // tokens
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kRawPlane = kTile * kCodeRow;         // 4 KB of codes
@@ -59,16 +63,22 @@ constexpr int kRawMeta = 2 * kRawPlane;             // V scale[32] | V zero[32]
 constexpr int kRawBytes = kRawMeta + 2 * kTile * 4;
 constexpr int kFragBytes = 8 * 1024;                // a tile's 8 fragments of K, or of V
 constexpr int kFragsV = 3;                          // V's buffers; K's are two
-constexpr int kDepth = 4;                           // tiles whose copies are in flight or not converted yet
+constexpr int kDepth = 4;                           // steps whose copies are in flight or not converted yet
 constexpr float kSlack = 8.0f;                      // log2 units that the reference may lag behind
 
-template <int LAYOUT>
+// TS: tiles of a step, one for each TS-th of the wavefronts.
+template <int LAYOUT, int TS>
 __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<kWorkUnit> &seg, int h, int chunk,
                                              const int tid) {
     const int Hkv = a.geo.Hkv;
-    const int lane = tid & 63, w = tid >> 6, col = lane & 15, kg = lane >> 4;
+    constexpr int kRows = kWideRows / TS;
+    constexpr int kTilesPerGroup = kKGroup / kTile;
+    static_assert(kTilesPerGroup % (2 * TS) == 0, "two steps stay in one K group");
+    constexpr int kSteps = kTilesPerGroup / TS;  // per group
+    const int lane = tid & 63, w = __builtin_amdgcn_readfirstlane(tid >> 6), col = lane & 15, kg = lane >> 4;
     const int b = seg.b, T = seg.T, g0 = seg.g0;
-    const int row0 = chunk * kRows + 32 * w;  // of the wavefront
+    const int ts = w / (kWaves / TS);                            // the wavefront's tile of a step
+    const int row0 = chunk * kRows + 32 * (w % (kWaves / TS));  // its rows
     auto partial_index = [&](int r) { return ((size_t)h * a.rows_total + r) * a.n_seg + seg.number; };
     if (seg.n_groups == 0) {  // an empty sequence: (max, sum) = (-inf, 0)
         for (int r = chunk * kRows + tid; r < min(a.rows_total, (chunk + 1) * kRows); r += kThreads)
@@ -76,15 +86,15 @@ __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<
         return;
     }
     const int first = g0 * kKGroup, end = min(T, first + seg.n_groups * kKGroup);
-    const int n_tiles = (end - first + kTile - 1) / kTile;
+    const int n_steps = (end - first + kTile * TS - 1) / (kTile * TS);
 
-    __shared__ __attribute__((aligned(16))) uint8_t s_raw[kDepth][kRawBytes];
-    __shared__ __attribute__((aligned(16))) uint8_t s_frag[2 + kFragsV][kFragBytes];
+    __shared__ __attribute__((aligned(16))) uint8_t s_raw[kDepth][TS][kRawBytes];
+    __shared__ __attribute__((aligned(16))) uint8_t s_frag[2 + kFragsV][TS][kFragBytes];
     __shared__ __attribute__((aligned(16))) float s_km[2][2 * kHeadDim];  // K scale | zero of a group, two groups
-    __shared__ int32_t s_ids[LAYOUT == 0 ? 1 : kWaves][2 * kDepth][8];  // blocks of a tile's rows
+    __shared__ int32_t s_ids[LAYOUT == 0 ? 1 : kWaves][2 * kDepth][TS][8];  // blocks of a step's rows
     __shared__ int s_e[kHeadDim];                                       // channel exponents
     __shared__ float s_vmax[kWaves];
-    float(*s_max)[kHeadDim] = reinterpret_cast<float(*)[kHeadDim]>(&s_frag[0][0]);  // (before there are fragments)
+    float(*s_max)[kHeadDim] = reinterpret_cast<float(*)[kHeadDim]>(&s_frag[0][0][0]);  // (before there are fragments)
     auto frag_k = [&](int j) { return s_frag[j & 1]; };
     auto frag_v = [&](int j) { return s_frag[2 + j % kFragsV]; };
 
@@ -97,48 +107,67 @@ __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<
     // A row per 8 lanes; lane l fills physical chunk l % 8 of its row.
     const int crow = lane >> 3;
     auto block_of = [&](int t) { return a.bt_shift >= 0 ? t >> a.bt_shift : t / a.geo.bt; };
-    auto token_of = [&](int j, int k) { return min(first + kTile * j + 8 * (k & 3) + crow, T - 1); };
-    auto block_at = [&](int j) { return LAYOUT == 0 ? bt_row : bt_row + block_of(token_of(j, w)); };
-    // Every wavefront issues as many operations per tile, so that it can wait for
-    // the older ones: a copy of rows, one of metadata (K's with a group's
-    // first tile, by wavefront 1; else V's, which may be written more than once),
-    // and the block numbers of a later tile.
+    auto token_of = [&](int j, int k) { return min(first + kTile * (TS * j + k) + 8 * (w & 3) + crow, T - 1); };
+    // Every wavefront issues as many operations per step, so that it can wait for
+    // the older ones: for each tile a copy of rows, one of metadata (K's with a
+    // group's first step, by wavefront TS; else V's of tile w % TS, which may be
+    // written more than once), and the block numbers of a later step.
     // Wavefront w copies rows 8 (w % 4) .. + 7 of K (w < 4) or V.
-    constexpr int kOps = LAYOUT == 0 ? 2 : 3;
+    constexpr int kOps = TS + (LAYOUT == 0 ? 1 : 2);
     auto copy_ids = [&](int j) {
-        if (LAYOUT != 0 && lane < 8) {
-            const int t = min(first + kTile * j + 8 * (w & 3) + lane, T - 1);
-            lds_copy4(bt_row + block_of(t), lds_addr(&s_ids[LAYOUT == 0 ? 0 : w][j % (2 * kDepth)][0]));
+        if (LAYOUT != 0 && lane < 8 * TS) {
+            const int t = min(first + kTile * (TS * j + (lane >> 3)) + 8 * (w & 3) + (lane & 7), T - 1);
+            lds_copy4(bt_row + block_of(t), lds_addr(&s_ids[LAYOUT == 0 ? 0 : w][j % (2 * kDepth)][0][0]));
         }
     };
-    auto issue = [&](int j, int id) {
-        if (j >= n_tiles) return;
-        const uint32_t slot = lds_addr(s_raw[j % kDepth]);
-        const int t = token_of(j, w);
-        if (id < 0 || id >= a.geo.num_blocks) {
-            bad = true;
-            id = 0;
+    // logical chunk of the physical one that the lane fills, in bytes
+    const uint32_t chunk_off = 16u * (uint32_t)((lane & 7) ^ crow ^ (w < 4 ? 0 : ((w & 3) >> 1) << 2));
+    const int id0 = LAYOUT == 0 ? bt_row[0] : 0;
+    if (LAYOUT == 0) bad = id0 < 0 || id0 >= a.geo.num_blocks;
+    const size_t blk0 = ((size_t)(bad ? 0 : id0) * Hkv + h) * a.geo.bt;  // (LAYOUT 0) the sequence's first row
+    const uint32_t km0 = lds_addr(&s_km[0][0]);
+    const uint32_t raw0 = lds_addr(&s_raw[0][0][0]);
+    auto raw_of = [&](int j, int k) { return raw0 + (uint32_t)((j % kDepth) * TS + k) * kRawBytes; };
+    auto issue = [&](int j, auto id_of) {
+        if (j >= n_steps) return;
+#pragma unroll
+        for (int k = 0; k < TS; ++k) {
+            const uint8_t *codes = w < 4 ? a.k_codes : a.v_codes;
+            if (LAYOUT == 0) {  // rows side by side: the first one's address is the wavefront's
+                const int t = min(first + kTile * (TS * j + k) + 8 * (w & 3), T - 1);
+                lds_copy16(codes + (blk0 + t) * kCodeRow, (uint32_t)(min(crow, T - 1 - t) * kCodeRow) + chunk_off,
+                           raw_of(j, k) + 1024u * w);
+                continue;
+            }
+            const int t = token_of(j, k);
+            int id = id_of(k);
+            if (id < 0 || id >= a.geo.num_blocks) {
+                bad = true;
+                id = 0;
+            }
+            const size_t row = ((size_t)id * Hkv + h) * a.geo.bt + (size_t)(t - block_of(t) * a.geo.bt);
+            lds_copy16(codes + row * kCodeRow + chunk_off, raw_of(j, k) + 1024u * w);
         }
-        const size_t row = ((size_t)id * Hkv + h) * a.geo.bt + (size_t)(LAYOUT == 0 ? t : t - block_of(t) * a.geo.bt);
-        const int q = (lane & 7) ^ crow ^ (w < 4 ? 0 : ((w & 3) >> 1) << 2);
-        lds_copy16((w < 4 ? a.k_codes : a.v_codes) + row * kCodeRow + 16 * q, slot + 1024u * w);
-        if (w == 1 && (j & 3) == 0) {
-            lds_copy16((lane < 32 ? a.meta.k_scale : a.meta.k_zero) + kmeta + (size_t)(g0 + (j >> 2)) * kHeadDim + 4 * (lane & 31),
-                       lds_addr(s_km[(j >> 2) & 1]));
+        if (w == TS && j % kSteps == 0) {
+            const int g = j / kSteps;
+            lds_copy16((lane < 32 ? a.meta.k_scale : a.meta.k_zero) + kmeta + (size_t)(g0 + g) * kHeadDim + 4 * (lane & 31),
+                       km0 + (uint32_t)(g & 1) * 2 * kHeadDim * 4);
         } else {
-            const int tt = min(first + kTile * j + (lane & 31), T - 1);
-            lds_copy4((lane < 32 ? a.meta.v_scale : a.meta.v_zero) + vmeta + tt, slot + kRawMeta);
+            const int tt = min(first + kTile * (TS * j + w % TS) + (lane & 31), T - 1);
+            lds_copy4((lane < 32 ? a.meta.v_scale : a.meta.v_zero) + vmeta + tt, raw_of(j, w % TS) + kRawMeta);
         }
         copy_ids(j + kDepth);
     };
 
     // ---- the exponents of the segment's channels and of its values ----
     {
-        int ids[kDepth];
+        int ids[kDepth][TS];
 #pragma unroll
-        for (int j = 0; j < kDepth; ++j) ids[j] = *block_at(min(j, n_tiles - 1));
+        for (int j = 0; j < kDepth; ++j)
 #pragma unroll
-        for (int j = 0; j < kDepth; ++j) issue(j, ids[j]);
+            for (int k = 0; k < TS; ++k) ids[j][k] = LAYOUT == 0 ? 0 : bt_row[block_of(token_of(j, k))];
+#pragma unroll
+        for (int j = 0; j < kDepth; ++j) issue(j, [&](int k) { return ids[j][k]; });
     }
     {
         float4 m = make_float4(0.f, 0.f, 0.f, 0.f);
@@ -223,7 +252,7 @@ __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<
         sc[rt] = __builtin_amdgcn_fmed3f(ldexpf(kLog2e * rsqrtf((float)kHeadDim), E), FLT_MIN, FLT_MAX);
     }
 
-    // ---- conversion of a tile into operand order ----
+    // ---- conversion of a step into operand order ----
     // K: fragment 4 r + kk: lane (token 16 r + col, dims 32 kk + 8 kg .. + 7); V:
     // fragment c: lane (dim 16 c + col, tokens 16 (e / 4) + 4 kg + e % 4).  Wavefront
     // w makes fragment w of each.
@@ -233,84 +262,102 @@ __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<
 #pragma unroll
         for (int e = 0; e < 8; ++e) {
             const int d = 32 * kk_own + 8 * kg + e;
-            const float sc = ldexpf(s_km[(j >> 2) & 1][d], -s_e[d]);
+            const float *km = s_km[(j / kSteps) & 1];
+            const float sc = ldexpf(km[d], -s_e[d]);
             ks[e / 2][e % 2] = (_Float16)sc;
-            kz[e / 2][e % 2] = (_Float16)fmaf(128.0f, sc, ldexpf(s_km[(j >> 2) & 1][kHeadDim + d], -s_e[d]));
+            kz[e / 2][e % 2] = (_Float16)fmaf(128.0f, sc, ldexpf(km[kHeadDim + d], -s_e[d]));
         }
     };
     const float down = ldexpf(1.0f, -Ev);
-    auto convert = [&](int j) {  // (of a tile past the last: what its slot holds, to where nothing reads)
-        const uint8_t *raw = s_raw[j % kDepth];
-        {
-            const int t = 16 * (w >> 2) + col, q = 2 * kk_own + (kg >> 1);
-            const uint2 c = *reinterpret_cast<const uint2 *>(raw + t * kCodeRow + ((q ^ (t & 7)) * 16) + 8 * (kg & 1));
-            u32x4_t o;
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                // a byte under 0x64 is 1024 + code
-                const uint32_t code = __builtin_amdgcn_perm(0x64646464u, e < 2 ? c.x : c.y, e & 1 ? 0x04030402u : 0x04010400u);
-                const h2 x = __builtin_bit_cast(h2, code) - (h2){(_Float16)1152.0f, (_Float16)1152.0f};
-                o[e] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(x, ks[e], kz[e]));
-            }
-            *reinterpret_cast<u32x4_t *>(frag_k(j) + w * 1024 + 16 * lane) = o;
-        }
-        const float *vm = reinterpret_cast<const float *>(raw + kRawMeta) + 4 * kg;
-        const float4 s0 = *reinterpret_cast<const float4 *>(vm), s1 = *reinterpret_cast<const float4 *>(vm + 16);
-        const float4 z0 = *reinterpret_cast<const float4 *>(vm + kTile), z1 = *reinterpret_cast<const float4 *>(vm + kTile + 16);
-        const float vs[8] = {s0.x, s0.y, s0.z, s0.w, s1.x, s1.y, s1.z, s1.w};
-        const float vz[8] = {z0.x, z0.y, z0.z, z0.w, z1.x, z1.y, z1.z, z1.w};
+    // (of a step past the last: what its slot holds, to where nothing reads)
+    struct Raw {
+        uint2 k;
+        intx2_t v;
+        float4 s[2], z[2];
+    };
+    auto load_raw = [&](int j, int k) {
+        const int t = 16 * (w >> 2) + col, q = 2 * kk_own + (kg >> 1);
         const int tr = 16 * ((col >> 1) >> 2) + 4 * kg + ((col >> 1) & 3);
-        {
-            const intx2_t v = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
-                (__attribute__((address_space(3))) intx2_t *)(raw + kRawPlane + v_slot(tr, w) + 8 * (col & 1)));
-            u32x4_t o;
+        const uint8_t *p = s_raw[j % kDepth][k];
+        const float *vm = reinterpret_cast<const float *>(p + kRawMeta) + 4 * kg;
+        Raw r;
+        r.k = *reinterpret_cast<const uint2 *>(p + t * kCodeRow + ((q ^ (t & 7)) * 16) + 8 * (kg & 1));
+        r.v = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
+            (__attribute__((address_space(3))) intx2_t *)(p + kRawPlane + v_slot(tr, w) + 8 * (col & 1)));
 #pragma unroll
-            for (int e = 0; e < 8; e += 2) {
-                const uint32_t x = (uint32_t)v[e >> 2] >> (8 * (e & 3));
-                o[e / 2] = pack_f16_rne(down * fmaf((float)(x & 0xFFu), vs[e], vz[e]),
-                                        down * fmaf((float)((x >> 8) & 0xFFu), vs[e + 1], vz[e + 1]));
-            }
-            *reinterpret_cast<u32x4_t *>(frag_v(j) + w * 1024 + 16 * lane) = o;
+        for (int i = 0; i < 2; ++i) {
+            r.s[i] = *reinterpret_cast<const float4 *>(vm + 16 * i);
+            r.z[i] = *reinterpret_cast<const float4 *>(vm + kTile + 16 * i);
         }
+        return r;
+    };
+    auto convert = [&](int j, int k, const Raw &raw) {
+        u32x4_t o;
+#pragma unroll
+        for (int e = 0; e < 4; ++e) {
+            // a byte under 0x64 is 1024 + code
+            const uint32_t code =
+                __builtin_amdgcn_perm(0x64646464u, e < 2 ? raw.k.x : raw.k.y, e & 1 ? 0x04030402u : 0x04010400u);
+            const h2 x = __builtin_bit_cast(h2, code) - (h2){(_Float16)1152.0f, (_Float16)1152.0f};
+            o[e] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(x, ks[e], kz[e]));
+        }
+        *reinterpret_cast<u32x4_t *>(frag_k(j)[k] + w * 1024 + 16 * lane) = o;
+        const float4 *s = raw.s, *z = raw.z;
+        const float vs[8] = {s[0].x, s[0].y, s[0].z, s[0].w, s[1].x, s[1].y, s[1].z, s[1].w};
+        const float vz[8] = {z[0].x, z[0].y, z[0].z, z[0].w, z[1].x, z[1].y, z[1].z, z[1].w};
+#pragma unroll
+        for (int e = 0; e < 8; e += 2) {
+            const uint32_t x = (uint32_t)raw.v[e >> 2] >> (8 * (e & 3));
+            o[e / 2] = pack_f16_rne(down * fmaf((float)(x & 0xFFu), vs[e], vz[e]),
+                                    down * fmaf((float)((x >> 8) & 0xFFu), vs[e + 1], vz[e + 1]));
+        }
+        *reinterpret_cast<u32x4_t *>(frag_v(j)[k] + w * 1024 + 16 * lane) = o;
     };
 
     wait_vmcnt<0>();
     __syncthreads();
     load_group(0);
-    convert(0);
-    if (n_tiles > 1) convert(1);
-    float m_run[2] = {-INFINITY, -INFINITY}, l[2] = {0.0f, 0.0f};
-    f32x4_t acc[2][8];
+    for (int j = 0; j < min(n_steps, 2); ++j)
+        for (int k = 0; k < TS; ++k) convert(j, k, load_raw(j, k));
+    // the reference (-FLT_MAX while no token has been seen: a number, so that -inf
+    // less it is -inf), and where it follows
+    float m_run[2] = {-FLT_MAX, -FLT_MAX}, follow[2] = {-FLT_MAX, -FLT_MAX};
+    f32x4_t acc[2][8], l[2] = {};  // l: the sums of the weights, a ninth column of the values, all ones
+    const u32x4_t ones = {0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u};
 #pragma unroll
     for (int rt = 0; rt < 2; ++rt)
 #pragma unroll
         for (int c = 0; c < 8; ++c) acc[rt][c] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     // (a wavefront without rows computes its last one over: a branch around the
-    // products costs the others more, 417 us against 361 where all have rows)
+    // products cost the others more, 417 us against 361 where all have rows)
     const bool rows_live = row0 < a.rows_total;  // uniform in the wavefront
-    const int id0 = LAYOUT == 0 ? bt_row[0] : 0;
-    asm volatile("" ::"s"(id0));  // in before the copies go on
     __syncthreads();
     f32x4_t s[2][2];
-    auto scores = [&](int j, f32x4_t (&x)[2][2]) {
-        const uint8_t *frag = frag_k(j) + 16 * lane;
+    auto load_frags = [&](const uint8_t *frag, u32x4_t (&x)[8]) {
 #pragma unroll
-        for (int r = 0; r < 2; ++r) {
+        for (int c = 0; c < 8; ++c) x[c] = *reinterpret_cast<const u32x4_t *>(frag + c * 1024 + 16 * lane);
+    };
+    auto scores = [&](const u32x4_t (&k)[8], f32x4_t (&x)[2][2]) {
+#pragma unroll
+        for (int r = 0; r < 2; ++r)
 #pragma unroll
             for (int rt = 0; rt < 2; ++rt) x[rt][r] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
-            for (int kk = 0; kk < 4; ++kk) {
-                const u32x4_t k = *reinterpret_cast<const u32x4_t *>(frag + (4 * r + kk) * 1024);
+        for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
-                for (int rt = 0; rt < 2; ++rt) x[rt][r] = mfma_f16(k, qf[rt][kk], x[rt][r]);
-            }
-        }
+            for (int r = 0; r < 2; ++r)
+#pragma unroll
+                for (int rt = 0; rt < 2; ++rt) x[rt][r] = mfma_f16(k[4 * r + kk], qf[rt][kk], x[rt][r]);
     };
-    scores(0, s);
-    for (int j = 0; j < n_tiles; ++j) {
-        issue(j + kDepth, LAYOUT == 0 ? id0 : s_ids[LAYOUT == 0 ? 0 : w][(j + kDepth) % (2 * kDepth)][crow]);
-        if (((j + 2) & 3) == 0) load_group(j + 2);
-        const int t0 = first + kTile * j;
+    u32x4_t kf[8], vf[8];
+    load_frags(frag_k(0)[ts], kf);
+    scores(kf, s);
+    for (int j = 0; j < n_steps; ++j) {
+        issue(j + kDepth, [&](int k) {
+            return LAYOUT == 0 ? 0 : s_ids[LAYOUT == 0 ? 0 : w][(j + kDepth) % (2 * kDepth)][k][crow];
+        });
+        if ((j + 2) % kSteps == 0) load_group(j + 2);
+        const int t0 = first + kTile * (TS * j + ts);
         if (t0 + kTile > end) {
 #pragma unroll
             for (int r = 0; r < 2; ++r)
@@ -327,102 +374,168 @@ __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<
             const f32x4_t &x = s[rt][0], &y = s[rt][1];
             top[rt] = fmax3(fmax3(x[0], x[1], x[2]), fmax3(x[3], y[0], y[1]), fmax2(y[2], y[3])) * sc[rt];
         }
-        if (__any(top[0] > m_run[0] + kSlack || top[1] > m_run[1] + kSlack)) {
+        if (__any(top[0] > follow[0] || top[1] > follow[1])) {
 #pragma unroll
             for (int rt = 0; rt < 2; ++rt) {
                 const float m = fmaxf(max_kg(top[rt]), m_run[rt]);
-                const float alpha = m_run[rt] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_run[rt] - m);
+                const float alpha = __builtin_amdgcn_exp2f(m_run[rt] - m);
                 m_run[rt] = m;
-                l[rt] *= alpha;
+                follow[rt] = m + kSlack;
                 float af[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) af[i] = __shfl(alpha, 4 * kg + i);
+#pragma unroll
+                for (int i = 0; i < 4; ++i) l[rt][i] *= af[i];
 #pragma unroll
                 for (int c = 0; c < 8; ++c)
 #pragma unroll
                     for (int i = 0; i < 4; ++i) acc[rt][c][i] *= af[i];
             }
         }
-        // one stretch without branches from here
+        // Two stretches without branches, matrix and vector instructions in turns:
+        // the scores of the next step with this one's weights ...
+        load_frags(frag_k(j + 1)[ts], kf);
+        __builtin_amdgcn_sched_barrier(0);
+        load_frags(frag_v(j)[ts], vf);
         f32x4_t ahead[2][2];
-        scores(j + 1, ahead);
+        scores(kf, ahead);
         u32x4_t pa[2];
 #pragma unroll
         for (int rt = 0; rt < 2; ++rt) {
             const f32x4_t &x = s[rt][0], &y = s[rt][1];
-            const float ref = m_run[rt] == -INFINITY ? 0.0f : -m_run[rt];
             float p[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) {
-                p[i] = __builtin_amdgcn_exp2f(fmaf(i < 4 ? x[i & 3] : y[i & 3], sc[rt], ref));
-                l[rt] += p[i];
-            }
+            for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(i < 4 ? x[i & 3] : y[i & 3], sc[rt], -m_run[rt]));
 #pragma unroll
             for (int e = 0; e < 4; ++e) pa[rt][e] = pack_f16_rne(p[2 * e], p[2 * e + 1]);
         }
-        const uint8_t *frag = frag_v(j) + 16 * lane;
 #pragma unroll
-        for (int c = 0; c < 8; ++c) {
-            const u32x4_t v = *reinterpret_cast<const u32x4_t *>(frag + c * 1024);
-#pragma unroll
-            for (int rt = 0; rt < 2; ++rt) acc[rt][c] = mfma_f16(pa[rt], v, acc[rt][c]);
+        for (int i = 0; i < 16; ++i) {
+            __builtin_amdgcn_sched_group_barrier(0x8, 1, 0);
+            __builtin_amdgcn_sched_group_barrier(0x2, 3, 0);
+            if (i >= 4 && i < 12) __builtin_amdgcn_sched_group_barrier(0x100, 1, 0);
         }
-        convert(j + 2);
+        __builtin_amdgcn_sched_barrier(0);
+        // ... the values, and the conversions: tile k with its share of the products
+#pragma unroll
+        for (int k = 0; k < TS; ++k) {
+            const Raw raw = load_raw(j + 2, k);
+#pragma unroll
+            for (int c = 8 / TS * k; c < 8 / TS * (k + 1); ++c)
+#pragma unroll
+                for (int rt = 0; rt < 2; ++rt) acc[rt][c] = mfma_f16(pa[rt], vf[c], acc[rt][c]);
+            if (k == TS - 1)
+#pragma unroll
+                for (int rt = 0; rt < 2; ++rt) l[rt] = mfma_f16(pa[rt], ones, l[rt]);
+            convert(j + 2, k, raw);
+            __builtin_amdgcn_sched_group_barrier(0x100, 6, 1);
+            constexpr int kFirst = 4;  // products that run while the codes come in
+            __builtin_amdgcn_sched_group_barrier(0x8, kFirst, 1);
+#pragma unroll
+            for (int i = 0; i < 16 / TS - kFirst; ++i) {
+                __builtin_amdgcn_sched_group_barrier(0x2, 4 * TS, 1);
+                __builtin_amdgcn_sched_group_barrier(0x8, 1, 1);
+            }
+            __builtin_amdgcn_sched_barrier(0);
+        }
 #pragma unroll
         for (int rt = 0; rt < 2; ++rt)
 #pragma unroll
             for (int r = 0; r < 2; ++r) s[rt][r] = ahead[rt][r];
-        // tile j + 3 is in once only the later ones' operations are in flight
-        static_assert(kDepth == 4, "one tile's may be");
-        if (j + kDepth < n_tiles)
+        // step j + 3 is in once only the later ones' operations are in flight
+        static_assert(kDepth == 4, "one step's may be");
+        if (j + kDepth < n_steps)
             wait_vmcnt<kOps>();
         else
             wait_vmcnt<0>();
         __syncthreads();
     }
 
-    // ---- the partials: through LDS, so that rows are written whole ----
+    // ---- the partials ----
     const bool any_bad = __syncthreads_or(bad);
-    if (!rows_live) return;
-    float *s_o = reinterpret_cast<float *>(&s_frag[0][0]) + (size_t)w * 8 * (kHeadDim + 4);  // 8 rows of the wavefront
-    static_assert(kWaves * 8 * (kHeadDim + 4) * 4 <= (2 + kFragsV) * kFragBytes, "the rows must fit in the operands' place");
     const float up = ldexpf(1.0f, Ev);
+    // Of row tile rt, through LDS, so that rows are written whole: 8 rows of the
+    // wavefront at a time.
+    float *s_o = reinterpret_cast<float *>(&s_frag[0][0][0]) + (size_t)w * 8 * (kHeadDim + 4);
+    static_assert(kWaves * 8 * (kHeadDim + 4) * 4 <= (2 + kFragsV) * kFragBytes, "the rows must fit in the operands' place");
+    auto write_tile = [&](int rt, float m, f32x4_t l4, const f32x4_t (&o)[8]) {
+        float sum = 0.0f;  // of row col: element col % 4 of the lanes of kg = col / 4
 #pragma unroll
-    for (int rt = 0; rt < 2; ++rt) {
-        const float sum = any_bad ? NAN : sum_kg(l[rt]);
+        for (int i = 0; i < 4; ++i) {
+            const float x = __shfl(l4[i], 16 * (col >> 2));
+            sum = (col & 3) == i ? x : sum;
+        }
+        if (any_bad) sum = NAN;
         const int r = row0 + 16 * rt + col;
         if (kg == 0 && r < a.rows_total) {
-            const f32x2_t ml = {m_run[rt], sum};
+            const f32x2_t ml = {m == -FLT_MAX ? -INFINITY : m, sum};
             __builtin_nontemporal_store(ml, reinterpret_cast<f32x2_t *>(a.ws_ml + partial_index(r)));
         }
 #pragma unroll
         for (int half = 0; half < 2; ++half) {
-            // rows 4 kg + 2 half, + 1 of the tile: 8 rows at a time
+            // rows 4 kg + 2 half, + 1 of the tile
 #pragma unroll
             for (int i = 0; i < 2; ++i)
 #pragma unroll
-                for (int c = 0; c < 8; ++c) s_o[(2 * kg + i) * (kHeadDim + 4) + 16 * c + col] = acc[rt][c][2 * half + i] * up;
+                for (int c = 0; c < 8; ++c) s_o[(2 * kg + i) * (kHeadDim + 4) + 16 * c + col] = o[c][2 * half + i] * up;
             __builtin_amdgcn_wave_barrier();
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
 #pragma unroll
             for (int k = 0; k < 4; ++k) {
                 const int lr = 2 * k + (lane >> 5);  // row 4 (lr / 2) + 2 half + lr % 2 of the tile
                 const int row = row0 + 16 * rt + 4 * (lr >> 1) + 2 * half + (lr & 1);
-                f32x4_t o = *reinterpret_cast<const f32x4_t *>(s_o + lr * (kHeadDim + 4) + 4 * (lane & 31));
-                if (any_bad) o = f32x4_t{NAN, NAN, NAN, NAN};
+                f32x4_t x = *reinterpret_cast<const f32x4_t *>(s_o + lr * (kHeadDim + 4) + 4 * (lane & 31));
+                if (any_bad) x = f32x4_t{NAN, NAN, NAN, NAN};
                 if (row < a.rows_total)
                     __builtin_nontemporal_store(
-                        o, reinterpret_cast<f32x4_t *>(a.ws_o + partial_index(row) * kHeadDim) + (lane & 31));
+                        x, reinterpret_cast<f32x4_t *>(a.ws_o + partial_index(row) * kHeadDim) + (lane & 31));
             }
             asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
             __builtin_amdgcn_wave_barrier();
         }
+    };
+    if constexpr (TS == 1) {
+        if (!rows_live) return;
+        write_tile(0, m_run[0], l[0], acc[0]);
+        write_tile(1, m_run[1], l[1], acc[1]);
+    } else {
+        // Two wavefronts have the same rows: each gives the other what it has of
+        // one row tile (ts 0 of tile 1, ts 1 of tile 0) and writes the other tile.
+        const bool one = ts != 0;
+        f32x4_t *s_x = reinterpret_cast<f32x4_t *>(&s_frag[0][0][0]);  // [wavefront][9][lane]
+        float *s_y = reinterpret_cast<float *>(&s_raw[0][0][0]);       // [wavefront][lane]
+        static_assert(kWaves * 9 * 64 * 16 <= (2 + kFragsV) * TS * kFragBytes, "the exchange must fit");
+#pragma unroll
+        for (int c = 0; c < 8; ++c) s_x[(w * 9 + c) * 64 + lane] = one ? acc[0][c] : acc[1][c];
+        s_x[(w * 9 + 8) * 64 + lane] = one ? l[0] : l[1];
+        s_y[w * 64 + lane] = one ? m_run[0] : m_run[1];
+        __syncthreads();
+        const int other = w ^ (kWaves / TS);
+        const float m_other = s_y[other * 64 + lane];
+        const float m_own = one ? m_run[1] : m_run[0], m = fmaxf(m_own, m_other);
+        const float f_own = __builtin_amdgcn_exp2f(m_own - m), f = __builtin_amdgcn_exp2f(m_other - m);
+        float fo[4], ft[4];
+#pragma unroll
+        for (int i = 0; i < 4; ++i) {
+            fo[i] = __shfl(f_own, 4 * kg + i);
+            ft[i] = __shfl(f, 4 * kg + i);
+        }
+        f32x4_t o[9];
+#pragma unroll
+        for (int c = 0; c < 9; ++c) {
+            const f32x4_t x = s_x[(other * 9 + c) * 64 + lane];
+            const f32x4_t y = c == 8 ? (one ? l[1] : l[0]) : one ? acc[1][c & 7] : acc[0][c & 7];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) o[c][i] = fmaf(x[i], ft[i], y[i] * fo[i]);
+        }
+        __syncthreads();  // the exchange is read
+        if (rows_live) write_tile(ts, m, o[8], reinterpret_cast<const f32x4_t(&)[8]>(o));
     }
 }
 
 // As verify.hip's kernels: grid (worker, kv head x chunk) for the contiguous
 // layout, the kv head fastest for paged ones.
-template <int LAYOUT, int FIND>
+template <int LAYOUT, int FIND, int TS>
 __global__ __launch_bounds__(kThreads, 2) void verify_wide_kernel(VerifyArgs a) {
     const int worker = LAYOUT == 0 ? blockIdx.x : blockIdx.y;
     const int hc = LAYOUT == 0 ? blockIdx.y : blockIdx.x;
@@ -430,37 +543,41 @@ __global__ __launch_bounds__(kThreads, 2) void verify_wide_kernel(VerifyArgs a) 
     Segment<kWorkUnit> seg;
     if (FIND == 0) {  // a unit per workgroup
         if (!seg.set_unit(a.seq_lens, a.max_seq_len, a.direct, blockIdx.z, worker)) return;
-        wide_segment<LAYOUT>(a, seg, h, chunk, threadIdx.x);
+        wide_segment<LAYOUT, TS>(a, seg, h, chunk, threadIdx.x);
         return;
     }
     const WorkList<kWorkUnit, true> list(a.seq_lens, a.B, a.max_seq_len, a.workers);
     if (!seg.start(list, worker)) return;
     for (;;) {
-        wide_segment<LAYOUT>(a, seg, fresh_uniform(h), fresh_uniform(chunk), fresh_tid());
+        wide_segment<LAYOUT, TS>(a, seg, fresh_uniform(h), fresh_uniform(chunk), fresh_tid());
         if (!seg.next(list, worker)) return;
         __syncthreads();  // the segment's LDS is free again
     }
 }
 
-template <int LAYOUT>
-void launch_find(const VerifyArgs &a, dim3 grid, hipStream_t stream) {
-    if (a.direct)
-        hipLaunchKernelGGL((verify_wide_kernel<LAYOUT, 0>), grid, dim3(kThreads), 0, stream, a);
+template <int TS>
+void launch_steps(const VerifyArgs &a, dim3 grid, hipStream_t stream) {
+    if (a.geo.max_blocks == 1 && a.direct)
+        hipLaunchKernelGGL((verify_wide_kernel<0, 0, TS>), grid, dim3(kThreads), 0, stream, a);
+    else if (a.geo.max_blocks == 1)
+        hipLaunchKernelGGL((verify_wide_kernel<0, 1, TS>), grid, dim3(kThreads), 0, stream, a);
+    else if (a.direct)
+        hipLaunchKernelGGL((verify_wide_kernel<1, 0, TS>), grid, dim3(kThreads), 0, stream, a);
     else
-        hipLaunchKernelGGL((verify_wide_kernel<LAYOUT, 1>), grid, dim3(kThreads), 0, stream, a);
+        hipLaunchKernelGGL((verify_wide_kernel<1, 1, TS>), grid, dim3(kThreads), 0, stream, a);
 }
 
 }  // namespace
 
-hipError_t launch_verify_wide(const VerifyArgs &a, hipStream_t stream) {
+hipError_t launch_verify_wide(const VerifyArgs &a, int rows, hipStream_t stream) {
     if (a.rows_total < 1 || a.workers < 1 || a.workers > 65535) return hipErrorInvalidValue;
-    const unsigned hc = (unsigned)(a.geo.Hkv * ((a.rows_total + kWideRows - 1) / kWideRows));
+    const unsigned hc = (unsigned)(a.geo.Hkv * ((a.rows_total + rows - 1) / rows));
     const unsigned n = a.direct ? a.direct : a.workers, nz = a.direct ? a.B : 1;
     const dim3 grid = a.geo.max_blocks == 1 ? dim3(n, hc, nz) : dim3(hc, n, nz);
-    if (a.geo.max_blocks == 1)
-        launch_find<0>(a, grid, stream);
+    if (rows == kWideRows)
+        launch_steps<1>(a, grid, stream);
     else
-        launch_find<1>(a, grid, stream);
+        launch_steps<2>(a, grid, stream);
     return hipGetLastError();
 }
 

@@ -65,7 +65,7 @@ def run(c, q, kn, vn, parents, out=None, ws=None, max_len=None, wide=None):
 
 
 def run_wide(c, q, kn, vn, parents, out, max_len, wide):
-    """The same with the context's kernel given."""
+    """The same with the context's kernel given: 0, 1 (wide) or 2 (half as wide)."""
     B, n, Hq, _ = q.shape
     ws = torch.zeros(64 << 20, dtype=torch.uint8, device="cuda")
     f = lynx.load().lynx_internal_verify_tree
@@ -75,7 +75,7 @@ def run_wide(c, q, kn, vn, parents, out, max_len, wide):
            torch.as_tensor(np.asarray(parents, np.int32)).cuda(), out, ws]
     lens, table, kc, vc, qd, kd, vd, pd, od, wd = (x.data_ptr() for x in dev)
     assert f(ctypes.byref(c.L.c()), B, Hq, n, max_len, lens, table, kc, vc, ctypes.byref(c.pool.meta.c()), qd, kd, vd, pd, od,
-             wd, ws.nbytes, torch.cuda.current_stream().cuda_stream, int(wide)) == 0
+             wd, ws.nbytes, torch.cuda.current_stream().cuda_stream, wide) == 0
     torch.cuda.synchronize()
     return out.float().cpu().numpy()
 
@@ -86,7 +86,7 @@ def want(c, q, kn, vn, parents, lens=None):
                             bits(kn), bits(vn), parents)
 
 
-@pytest.mark.parametrize("wide", [None, True])
+@pytest.mark.parametrize("wide", [None, 1, 2])
 @pytest.mark.parametrize("lens,Hkv,G,n,bt", [
     ([1], 1, 1, 1, None),
     ([0], 2, 4, 5, None),               # no context: the tree alone
@@ -110,12 +110,13 @@ def test_trees(lens, Hkv, G, n, bt, wide):
     assert_close(run(c, *x, parents, wide=wide), want(c, *x, parents), ATOL, RTOL, "tree")
 
 
-def test_a_wide_call():
+@pytest.mark.parametrize("T,n,wide", [(131072 + 77, 64, 1), (200_077, 32, 2)])
+def test_a_wide_call(T, n, wide):
     """A call that the rule gives to the wide kernel, against the other one."""
-    c = cache([131072 + 77], 2, 16)
-    x = inputs_of(c, 8, 64)
-    parents = random_parents(1, 64, seed=9)
-    got, wide, narrow = (run(c, *x, parents, wide=w) for w in (None, True, False))
+    c = cache([T], 2, 16)
+    x = inputs_of(c, 8, n)
+    parents = random_parents(1, n, seed=9)
+    got, wide, narrow = (run(c, *x, parents, wide=w) for w in (None, wide, 0))
     assert np.array_equal(got, wide)
     assert_close(wide, narrow, ATOL, RTOL * 2, "wide")
 
@@ -142,7 +143,7 @@ def wide_inputs(kind):
 
 
 @pytest.mark.parametrize("kind", ["k", "v", "groups"])
-@pytest.mark.parametrize("wide", [False, True])
+@pytest.mark.parametrize("wide", [0, 1, 2])
 def test_wide_ranges(kind, wide):
     c, q, kn, vn = wide_inputs(kind)
     parents = random_parents(2, 30, seed=4)
@@ -223,7 +224,7 @@ def test_lengths_past_the_bound_and_bad_blocks():
     c.table = c.table.clone()
     c.table[1, 3] = c.n_blocks  # of sequence 1 alone
     parents[1, 4] = -2
-    for wide in (None, True):
+    for wide in (None, 1, 2):
         got = run(c, *x, parents, wide=wide)
         assert np.isfinite(got[0]).all() and np.isnan(got[1, :4]).all() and (got[1, 4] == 0).all()
 
