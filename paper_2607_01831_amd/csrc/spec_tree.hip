@@ -23,7 +23,8 @@
 //  * tree_path_kernel follows the path, a workgroup per (vocabulary chunk,
 //    sequence): each publishes its chunk's best score (or sum of weights) of
 //    the row, waits until all chunks are in, and goes on to the child that they
-//    decide: a few microseconds a row, and nothing else is read.
+//    decide: a few microseconds a row, and nothing else is read (drawn, besides,
+//    a row that the draw's chunk makes likely to be the next).
 // 16 sequences of 63 nodes and 128256 entries, 4 kept (525 MB in all rows, 41 MB
 // on the paths): 93.6 us (5.6 TB/s) and 19.7 us, 3.4 us a row after the first.
 // A wait in tree_path_kernel is bounded: a workgroup that has waited too long
@@ -403,7 +404,7 @@ __global__ __launch_bounds__(kThreads) void tree_path_kernel(TreeAcceptArgs a) {
     __shared__ float s_x[SAMPLE ? (PER + 1) * kThreads : 1];
     constexpr int kEnd = -1, kLate = -2;
 
-    const Tree tree(a, b);  // (the first wavefront's is used)
+    const Tree tree(a, b);
     int at = -1, kept = 0, mine = -1, choice = -1;
     uint64_t done = 0;  // rows above 0 that this workgroup has read, a bit per node
     // Ends when f() holds, or with false after so many looks.
@@ -415,11 +416,10 @@ __global__ __launch_bounds__(kThreads) void tree_path_kernel(TreeAcceptArgs a) {
         return false;
     };
     float v[PER];
-    int row = 0;
+    int row = 0, held = -1;  // held: the row whose chunk is in v already
     for (;;) {
-        const float *x = a.scores + (r0 + row) * V;
         uint64_t *words = a.words + (r0 + row) * a.chunks;
-        load_chunk(x, lo, V, vec4, v);
+        if (held != row) load_chunk(a.scores + (r0 + row) * V, lo, V, vec4, v);
         const uint64_t word = chunk_word<SAMPLE>(v, lo, vec4, s_wave);
         if (tid == 0) agent_store(words + c, word);
         const float uniform = SAMPLE ? a.uniforms[r0 + row] : 0.0f;
@@ -451,6 +451,17 @@ __global__ __launch_bounds__(kThreads) void tree_path_kernel(TreeAcceptArgs a) {
             if (draw == c) {  // the draw falls into this chunk: the others wait for its entry
                 const int entry = drawn_entry<PER>(s_x, lo, s_left, before, sum);
                 if (entry >= 0) agent_store(&state[row].choice, entry + 2);
+            }
+            // while the entry comes in, the row that follows if it is the token of
+            // the first child that lies in the drawn chunk (16 sequences of 128256
+            // entries, 4 kept: 31.2 us, without 34.4)
+            const int from = draw * PER * kThreads;
+            const bool mine_may = tree.there && tree.up == row - 1 && tree.token - from >= 0 &&
+                                  tree.token - from < PER * kThreads;
+            const uint64_t may = draw >= 0 ? __ballot(mine_may) : 0ull;
+            if (may) {
+                held = __ffsll((long long)may);  // the child's number and 1
+                load_chunk(a.scores + (r0 + held) * V, lo, V, vec4, v);
             }
             if (w == 0) {
                 int got = 1;  // no weight at all: -1
@@ -546,16 +557,17 @@ size_t spec_tree_workspace(int B, int n, int vocab) {
 }
 
 // Which kernel: the rows at once while reading them all takes no longer than
-// following a path of a few rows.  Greedy, 63 nodes, 4 kept, 128256 entries:
-// 2 sequences (66 MB) 15.8 us, along the path 15.6; 4 (131 MB) 24.4 and 15.8; 16
-// (525 MB) 93.6 and 19.7.  Drawn, where a row on the path waits for its draw
-// too: 4 sequences 31.5 us and 31.7; 8 64.2 and 31.9.  (A path as long as the
-// tree is the other extreme: a chain of 63, all kept, 16 sequences: 224 us along
-// it, 97 at once.)  Chunks: 4096 entries where every row is read, 8192 along a
-// path (16 sequences 20.2 us, by 4096 25.2, by 16384 26.7).
+// following a path of a few rows; at once and along the path, us.  Greedy, 4 kept:
+// 12.8M entries in all rows 13.2 and 15.5, 16.4M 16.2 and 16.0, 24.6M 20.4 and 18.2,
+// 65.7M 43.2 and 17.1.  Drawn, where a row on the path waits for its draw too, 4
+// kept: 12.8M 19.3 and 30.0, 24.6M 26.2 and 28.8, 25.6M 31.8 and 30.7, 32.8M 32.3 and
+// 29.5, 65.7M 65.6 and 29.1.  (A path as long as the tree is the other extreme: a
+// chain of 63, all kept, 16 sequences: 224 us along it, 97 at once.)  Chunks: 4096
+// entries where every row is read, 8192 along a path (16 sequences 20.2 us, by 4096
+// 25.2, by 16384 26.7).
 TreeAcceptWay spec_tree_way(int B, int n, int vocab, bool drawn) {
     const long long entries = (long long)B * (n + 1) * vocab;
-    return TreeAcceptWay{entries <= (drawn ? 33554432ll : 16777216ll), 128};
+    return TreeAcceptWay{entries <= (drawn ? 27000000ll : 16777216ll), 128};
 }
 
 hipError_t launch_spec_accept_tree(TreeAcceptArgs a, int B, TreeAcceptWay way, void *workspace, hipStream_t stream) {
