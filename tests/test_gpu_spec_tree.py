@@ -192,3 +192,28 @@ def test_one_workspace_for_every_shape_in_graphs_too():
                 assert np.array_equal(x.cpu().numpy(), w)
             check(*c, ws=ws)
     assert int(ws.max()) == 0
+
+
+@pytest.mark.parametrize("drawn", [False, True])
+def test_calls_on_two_streams_at_once(drawn):
+    """Along the path, each with a workspace of its own: whoever has to wait too
+    long for the other's workgroups gives the same result."""
+    calls = []
+    for seed in (1, 2):
+        c = case(24, 11, 128256, seed, drawn, agree=0.9)
+        dev = [torch.as_tensor(np.ascontiguousarray(x)).cuda() for x in (c[0], c[1].astype(np.int32), c[2].astype(np.int32))]
+        if drawn:
+            dev.append(torch.as_tensor(c[3]).cuda())
+        out = [torch.full(s, -7, dtype=torch.int32, device="cuda") for s in ((24,), (24, 11), (24,))]
+        calls.append((dev, out, lynx.spec_tree_workspace(24, 11, 128256), torch.cuda.Stream(), tree.accept_tree(*c)))
+    f = lynx.lynx_spec_accept_tree_sample if drawn else lynx.lynx_spec_accept_tree_greedy
+    torch.cuda.synchronize()
+    note(f"two streams drawn={drawn}")
+    for _ in range(5):
+        for dev, out, ws, stream, _ in calls:
+            f(*dev, *out, ws, stream=stream)
+    torch.cuda.synchronize()
+    for _, out, ws, _, want in calls:
+        assert int(ws.max()) == 0
+        for x, w in zip(out, want):
+            assert np.array_equal(x.cpu().numpy(), w)

@@ -206,6 +206,21 @@ def test_values_stay_on_their_path(value, n):
                 assert np.array_equal(got[b, i], clean[b, i]), (b, i)
 
 
+@pytest.mark.parametrize("wide", [0, 1, 2])
+@pytest.mark.parametrize("value", [float("nan"), float("inf"), 3e38])
+def test_a_query_reaches_its_row_alone(value, wide):
+    """(The other rows of a wavefront may be computed the other way, by a running
+    maximum: their roundings move, inside the tolerance of either way.)"""
+    c = cache([700, 130], 2, 16)
+    q, kn, vn = inputs_of(c, 8, 20)
+    parents = random_parents(2, 20, seed=2)
+    clean = want(c, q, kn, vn, parents)
+    q[1, 5, 3] = value
+    got = run(c, q, kn, vn, parents, wide=wide)
+    got[1, 5, 3] = clean[1, 5, 3]
+    assert_close(got, clean, ATOL, RTOL, "others")
+
+
 def test_a_dominant_node_and_a_dominant_context():
     """Scores that leave one side no weight."""
     c = cache([1000], 2)
