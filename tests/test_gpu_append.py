@@ -1,6 +1,8 @@
 """Tokens appended to the cache: after any appends its planes and metadata are
 those of encoding the whole sequence at once, bit for bit (the oracle's encode
 and merge); reading back is fma(code, scale, zero) rounded to BF16."""
+import ctypes
+
 import numpy as np
 import pytest
 import torch
@@ -301,6 +303,54 @@ def test_read_back_out_of_range():
         want[2, :10] = True   # up to the capacity of 200
         want[4, 6:12] = True  # block 0's tokens are skipped
         assert torch.equal(touched, want)
+
+
+def test_blocks_past_four_gigabytes():
+    """The same calls with the sequence in the first and in the last blocks of a
+    pool whose planes are larger than 2^32 bytes: the same bits."""
+    T, Hkv, bt, n, blocks = 1000, 8, 16, 40, 270_000
+    per = -(-(T + 64) // bt)
+    L = lynx.Layout(num_kv_heads=Hkv, block_tokens=bt, max_blocks_per_seq=per, num_blocks=blocks, max_tokens=T + 64)
+    assert L.plane_bytes(128) > 2 ** 32 + per * bt * Hkv * 128
+    planes = [torch.empty(L.plane_bytes(128), dtype=torch.uint8, device="cuda") for _ in range(2)]
+    k, v = (x[None].cuda() for x in random_kv(T, Hkv, seed=3))
+    q, kn, vn = (random_bf16((1, n, h, 128), 5 + i).cuda() for i, h in enumerate((32, Hkv, Hkv)))
+    ints = lambda x: torch.tensor(x, dtype=torch.int32).cuda()  # noqa: E731
+    parents = ints(random_parents(1, n, seed=4).tolist())
+    f = lynx.load().lynx_internal_verify_tree
+    P, I = ctypes.c_void_p, ctypes.c_int32
+    f.argtypes = [P, I, I, I, I, P, P, P, P, P, P, P, P, P, P, P, ctypes.c_size_t, P, I]
+    results = []
+    for first in (0, blocks - per):
+        meta = lynx.Meta.empty(L, 1)
+        table = torch.arange(first, first + per, dtype=torch.int32, device="cuda").view(1, per)
+        ring = torch.zeros(1, 256, Hkv, 128, dtype=torch.bfloat16, device="cuda")
+        note(f"blocks from {first}")
+        lynx.lynx_kv_append(L, 1, T, ints([0]), ints([T]), None, table, k, v, ring, *planes, None, None, None, None, meta)
+        back = [torch.zeros(1, T, Hkv, 128, dtype=torch.bfloat16, device="cuda") for _ in range(2)]
+        lynx.lynx_kv_dequant(L, 1, T, ints([0]), ints([T]), table, *planes, meta, *back)
+        again = torch.zeros_like(ring)
+        lynx.lynx_kv_append_begin(L, 1, ints([T]), table, planes[0], meta, again)
+        torch.cuda.synchronize()
+        got = [*back, again, ring, meta.k_scale, meta.v_zero]
+        lens, ws = ints([T]), torch.zeros(64 << 20, dtype=torch.uint8, device="cuda")
+        for wide in (0, 1, 2):
+            out = torch.zeros_like(q)
+            dev = [lens, table, *planes, q, kn, vn, parents, out, ws]
+            lp, tp, kp, vp, qp, knp, vnp, pp, op, wp = (x.data_ptr() for x in dev)
+            assert f(ctypes.byref(L.c()), 1, 32, n, T, lp, tp, kp, vp, ctypes.byref(meta.c()), qp, knp, vnp, pp, op, wp,
+                     ws.nbytes, torch.cuda.current_stream().cuda_stream, wide) == 0
+            torch.cuda.synchronize()
+            got.append(out)
+        results.append([x.cpu() for x in got])
+    for x, y in zip(*results):
+        assert torch.equal(x, y)
+    # and what was read back is what was written: half a code's step (largest
+    # scale) and the rounding to BF16, 2^-8 of the value, which is at most the
+    # written one and that half step
+    half, written = results[0][4].max().item() / 2, k.cpu().float()
+    error = (results[0][0].float() - written).abs()
+    assert (error <= half * 1.001 + (written.abs() + half) * 2.0 ** -8).all()
 
 
 def step_inputs(B, n, Hq, Hkv, V, seed):
