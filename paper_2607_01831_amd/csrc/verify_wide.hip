@@ -22,7 +22,8 @@
 //    square of its terms times sqrt(128).
 //  * V' = (zero + code scale) 2^-Ev, Ev over the segment, rounded to 11 bits, as
 //    are the weights p <= 2^8 against a reference that follows the row's maximum
-//    once it is 2^8 behind; l is summed in fp32.
+//    once it is 2^8 behind; l sums the rounded weights, so that an output is a
+//    mean by them, in fp32.
 //
 // A step is a tile of 32 tokens for 256 rows, or, for half the rows, two tiles
 // with a wavefront's two partners each on one (TS 2; they join at the end).  A
