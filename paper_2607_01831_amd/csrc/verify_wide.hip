@@ -170,22 +170,47 @@ __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<
 #pragma unroll
         for (int j = 0; j < kDepth; ++j) issue(j, [&](int k) { return ids[j][k]; });
     }
+    // the wavefront's queries: row col of each row tile, dims 8 kg + 32 kk
+    uint4 qraw[2][4];
+#pragma unroll
+    for (int rt = 0; rt < 2; ++rt) {
+        const int r = min(row0 + 16 * rt + col, a.rows_total - 1);
+        const uint16_t *q = a.q + (((size_t)b * a.nq + r / a.G) * a.Hq + (size_t)h * a.G + r % a.G) * kHeadDim + 8 * kg;
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk) qraw[rt][kk] = *reinterpret_cast<const uint4 *>(q + 32 * kk);
+    }
     {
         float4 m = make_float4(0.f, 0.f, 0.f, 0.f);
         const int d4 = tid & 31, gg = tid >> 5;  // 4 channels; groups gg, gg + 2 kWaves, ...
-        for (int g = gg; g < seg.n_groups; g += kThreads / 32) {
-            const float4 s = reinterpret_cast<const float4 *>(a.meta.k_scale + kmeta + (size_t)(g0 + g) * kHeadDim)[d4];
-            const float4 z = reinterpret_cast<const float4 *>(a.meta.k_zero + kmeta + (size_t)(g0 + g) * kHeadDim)[d4];
-            m.x = fmax3_abs(m.x, z.x, fmaf(255.0f, s.x, z.x));
-            m.y = fmax3_abs(m.y, z.y, fmaf(255.0f, s.y, z.y));
-            m.z = fmax3_abs(m.z, z.z, fmaf(255.0f, s.z, z.z));
-            m.w = fmax3_abs(m.w, z.w, fmaf(255.0f, s.w, z.w));
+        // (several loads in flight; past the segment's end its last is read again)
+        for (int g1 = gg; g1 < seg.n_groups; g1 += 4 * 2 * kWaves) {
+            float4 s[4], z[4];
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                const size_t at = kmeta + (size_t)(g0 + min(g1 + 2 * kWaves * i, seg.n_groups - 1)) * kHeadDim;
+                s[i] = reinterpret_cast<const float4 *>(a.meta.k_scale + at)[d4];
+                z[i] = reinterpret_cast<const float4 *>(a.meta.k_zero + at)[d4];
+            }
+#pragma unroll
+            for (int i = 0; i < 4; ++i) {
+                m.x = fmax3_abs(m.x, z[i].x, fmaf(255.0f, s[i].x, z[i].x));
+                m.y = fmax3_abs(m.y, z[i].y, fmaf(255.0f, s[i].y, z[i].y));
+                m.z = fmax3_abs(m.z, z[i].z, fmaf(255.0f, s[i].z, z[i].z));
+                m.w = fmax3_abs(m.w, z[i].w, fmaf(255.0f, s[i].w, z[i].w));
+            }
         }
         reinterpret_cast<float4 *>(s_max[gg])[d4] = m;
         float v = 0.0f;
-        for (int t = first + tid; t < end; t += kThreads) {
-            const float s = a.meta.v_scale[vmeta + t], z = a.meta.v_zero[vmeta + t];
-            v = fmax3_abs(v, z, fmaf(255.0f, s, z));
+        for (int t1 = first + tid; t1 < end; t1 += 8 * kThreads) {
+            float s[8], z[8];
+#pragma unroll
+            for (int i = 0; i < 8; ++i) {
+                const size_t at = vmeta + min(t1 + kThreads * i, end - 1);
+                s[i] = a.meta.v_scale[at];
+                z[i] = a.meta.v_zero[at];
+            }
+#pragma unroll
+            for (int i = 0; i < 8; ++i) v = fmax3_abs(v, z[i], fmaf(255.0f, s[i], z[i]));
         }
         v = max_kg(row16_max(v));
         if (lane == 0) s_vmax[w] = v;
@@ -210,17 +235,15 @@ __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<
     }
     __syncthreads();
 
-    // ---- the wavefront's queries: row col of each row tile, dims 8 kg + 32 kk ----
+    // ---- the queries as operands ----
     u32x4_t qf[2][4];
     float sc[2];
 #pragma unroll
     for (int rt = 0; rt < 2; ++rt) {
-        const int r = min(row0 + 16 * rt + col, a.rows_total - 1);
-        const uint16_t *q = a.q + (((size_t)b * a.nq + r / a.G) * a.Hq + (size_t)h * a.G + r % a.G) * kHeadDim + 8 * kg;
         float y[4][8];
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) {
-            const uint4 u = *reinterpret_cast<const uint4 *>(q + 32 * kk);
+            const uint4 u = qraw[rt][kk];
             const uint32_t x[4] = {u.x, u.y, u.z, u.w};
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
