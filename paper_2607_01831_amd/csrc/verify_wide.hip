@@ -108,6 +108,9 @@ __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<
     // A row per 8 lanes; lane l fills physical chunk l % 8 of its row.
     const int crow = lane >> 3;
     auto block_of = [&](int t) { return a.bt_shift >= 0 ? t >> a.bt_shift : t / a.geo.bt; };
+    auto place_in = [&](int t) { return a.bt_shift >= 0 ? t & (a.geo.bt - 1) : t % a.geo.bt; };
+    // row numbers in 32 bits: 2^32 rows of codes would be 512 GB
+    const uint32_t block_rows = (uint32_t)Hkv * a.geo.bt, head_rows = (uint32_t)h * a.geo.bt;
     auto token_of = [&](int j, int k) { return min(first + kTile * (TS * j + k) + 8 * (w & 3) + crow, T - 1); };
     // Every wavefront issues as many operations per step, so that it can wait for
     // the older ones: for each tile a copy of rows, one of metadata (K's with a
@@ -146,8 +149,8 @@ __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<
                 bad = true;
                 id = 0;
             }
-            const size_t row = ((size_t)id * Hkv + h) * a.geo.bt + (size_t)(t - block_of(t) * a.geo.bt);
-            lds_copy16(codes + row * kCodeRow + chunk_off, raw_of(j, k) + 1024u * w);
+            lds_copy16(codes + (size_t)((uint32_t)id * block_rows + head_rows + place_in(t)) * kCodeRow + chunk_off,
+                       raw_of(j, k) + 1024u * w);
         }
         if (w == TS && j % kSteps == 0) {
             const int g = j / kSteps;
