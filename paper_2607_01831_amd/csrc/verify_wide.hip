@@ -243,36 +243,35 @@ __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<
     float sc[2];
 #pragma unroll
     for (int rt = 0; rt < 2; ++rt) {
-        float y[4][8];
+        uint32_t x[4][4];  // two queries each
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk) {
-            const uint4 u = qraw[rt][kk];
-            const uint32_t x[4] = {u.x, u.y, u.z, u.w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                y[kk][2 * e] = bf16_lo(x[e]);
-                y[kk][2 * e + 1] = bf16_hi(x[e]);
-            }
+            x[kk][0] = qraw[rt][kk].x;
+            x[kk][1] = qraw[rt][kk].y;
+            x[kk][2] = qraw[rt][kk].z;
+            x[kk][3] = qraw[rt][kk].w;
         }
-        // the exponent of the row's largest product with a key, in two steps: the
-        // products themselves may leave the range of fp32
-        int E = -20000;
-#pragma unroll
-        for (int kk = 0; kk < 4; ++kk)
-#pragma unroll
-            for (int e = 0; e < 8; ++e) {
-                int x = 0;
-                frexpf(y[kk][e], &x);
-                if (y[kk][e] != 0.0f) E = max(E, x + s_e[32 * kk + 8 * kg + e]);
-            }
-        E = max(E, __shfl_xor(E, 16));
-        E = max(E, __shfl_xor(E, 32));
+        // the exponent of the row's largest product with a key (an upper bound where
+        // the query is subnormal), from the exponents of both: the products
+        // themselves may leave the range of fp32
+        constexpr int kNone = -20000;
+        int E = kNone;
 #pragma unroll
         for (int kk = 0; kk < 4; ++kk)
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int d = 32 * kk + 8 * kg + 2 * e;
-                qf[rt][kk][e] = pack_f16_rne(ldexpf(y[kk][2 * e], s_e[d] - E), ldexpf(y[kk][2 * e + 1], s_e[d + 1] - E));
+                const int lo = (int)(x[kk][e] >> 7 & 0xFFu) + s_e[d], hi = (int)(x[kk][e] >> 23 & 0xFFu) + s_e[d + 1];
+                E = max(E, max(x[kk][e] & 0x7FFFu ? lo : kNone, x[kk][e] & 0x7FFF0000u ? hi : kNone));
+            }
+        E = max(E, __shfl_xor(E, 16));
+        E = max(E, __shfl_xor(E, 32)) - 126;
+#pragma unroll
+        for (int kk = 0; kk < 4; ++kk)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) {
+                const int d = 32 * kk + 8 * kg + 2 * e;
+                qf[rt][kk][e] = pack_f16_rne(ldexpf(bf16_lo(x[kk][e]), s_e[d] - E), ldexpf(bf16_hi(x[kk][e]), s_e[d + 1] - E));
             }
         // positive and finite: times the -inf of a token past the context it must
         // not be a NaN
