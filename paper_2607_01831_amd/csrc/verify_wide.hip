@@ -20,10 +20,13 @@
 //    |centre'| + |K'|), where the BF16 key was off by 2^-9 |K'| to begin with.  128
 //    such errors are independent: a score moves by some 2e-4 of the root mean
 //    square of its terms times sqrt(128).
-//  * V' = (zero + code scale) 2^-Ev, Ev over the segment, rounded to 11 bits, as
-//    are the weights p <= 2^8 against a reference that follows the row's maximum
-//    once it is 2^8 behind; l sums the rounded weights, so that an output is a
-//    mean by them, in fp32.
+//  * V' = (zero + code scale) 2^(15 - Ev), Ev the exponent of the segment's largest
+//    |V|, rounded to fp16: off by 2^-12 of itself, and by 2^-40 of the largest where
+//    it is a subnormal (the largest stands at fp16's upper end, 2^15, so that one
+//    token's large values leave the others their bits).
+//  * weights p <= 2^8 against a reference that follows the row's maximum once it is
+//    2^8 behind, rounded to 11 bits; l sums the rounded weights, so that an output is
+//    a mean by them, in fp32.
 //
 // A step is a tile of 32 tokens for 256 rows, or, for half the rows, two tiles
 // with a wavefront's two partners each on one (TS 2; they join at the end).  A
@@ -66,6 +69,7 @@ constexpr int kFragBytes = 8 * 1024;                // a tile's 8 fragments of K
 constexpr int kFragsV = 3;                          // V's buffers; K's are two
 constexpr int kDepth = 4;                           // steps whose copies are in flight or not converted yet
 constexpr float kSlack = 8.0f;                      // log2 units that the reference may lag behind
+constexpr int kUpper = 15;                          // fp16 operands reach up to 2^15
 
 // TS: tiles of a step, one for each TS-th of the wavefronts.
 template <int LAYOUT, int TS>
@@ -234,7 +238,7 @@ __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<
 #pragma unroll
         for (int i = 1; i < kWaves; ++i) v = fmax2(v, s_vmax[i]);
         if (v > 0.0f && v <= FLT_MAX) frexpf(v, &Ev);
-        Ev = min(max(Ev, -126), 126);  // 2^Ev and 2^-Ev are normal numbers
+        Ev = min(max(Ev, kUpper - 126), 126);  // 2^(Ev - kUpper) and its inverse are normal numbers
     }
     __syncthreads();
 
@@ -294,7 +298,7 @@ __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<
             kz[e / 2][e % 2] = (_Float16)fmaf(128.0f, sc, ldexpf(km[kHeadDim + d], -s_e[d]));
         }
     };
-    const float down = ldexpf(1.0f, -Ev);
+    const float down = ldexpf(1.0f, kUpper - Ev);
     // (of a step past the last: what its slot holds, to where nothing reads)
     struct Raw {
         uint2 k;
@@ -479,7 +483,7 @@ __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<
 
     // ---- the partials ----
     const bool any_bad = __syncthreads_or(bad);
-    const float up = ldexpf(1.0f, Ev);
+    const float up = ldexpf(1.0f, Ev - kUpper);
     // Of row tile rt, through LDS, so that rows are written whole: 8 rows of the
     // wavefront at a time.
     float *s_o = reinterpret_cast<float *>(&s_frag[0][0][0]) + (size_t)w * 8 * (kHeadDim + 4);

@@ -1,0 +1,113 @@
+"""Verification of a token tree over caches whose ranges differ: values that one
+token makes large, weights that are far below the largest, keys far from 0 or
+with one token far from the others.  The context's kernels against the fp64
+statement over the same codes.
+
+Tolerance, for every output element, from the arithmetic of the wide kernel.  With p
+the fp64 weights and o the fp64 output of a row:
+ * a key is off by at most 2^-12 of its group's range, or of itself in a channel whose
+   groups all reach from below 0 to above it, and by 2^-39 of the channel's largest
+   (the subnormals of fp16), a query by 2^-39 of the row's largest product; fp32 sums
+   of 128 products by 2^-21 of their terms (8 roundings on the way of any).  That is at most d in a score, and a row's output moves by at
+   most d e^2d sum_i p_i |v_i - o|;
+ * a weight is off by 2^-12 of itself and by 2^-33 of the largest one: the output by
+   sum_i (2^-12 p_i + min(p_i, 2^-33)) |v_i - o|;
+ * a value is off by 2^-12 of itself and 2^-39 of the segment's largest, weighted p;
+ * the output is rounded to BF16: 2^-8 of it.
+The other kernel (0) holds a token's weight times its V scale in fp16, against the
+largest scale: 2^-11 of p times the token's range of values, and none that are 2^20
+times apart; and a query times K scale in two fp16 parts: 2^-21 of the products with
+the group's range.  It takes part where these bounds hold."""
+import numpy as np
+import pytest
+import torch
+
+from oracle import dequant, tree
+from tests.gpu_cases import bits, build_cache, device_meta_to_oracle, random_bf16, random_kv
+from tests.test_gpu_tree import random_parents, run
+
+pytestmark = pytest.mark.gpu
+
+
+def f64(t):
+    return t.double().numpy()
+
+
+def reference(c, q, kn, vn, parents, wide):
+    """(outputs, tolerances), fp64 [B][n][Hq][128]."""
+    B, n, Hq, D = q.shape
+    G = Hq // c.Hkv
+    meta = device_meta_to_oracle(c)
+    out, tol = np.zeros((B, n, Hq, D)), np.zeros((B, n, Hq, D))
+    for b in range(B):
+        T = c.lens[b]
+        K, V = dequant("full", c.OL, b, T, c.table.numpy(), c.pool.k_codes.cpu().numpy(), c.pool.v_codes.cpu().numpy(), meta)
+        spread = 255.0 * np.asarray(meta.k_scale[b], np.float64)  # [Hkv][groups][128]
+        zero = np.asarray(meta.k_zero[b], np.float64)
+        around = ((zero <= 0) & (zero + spread >= 0))[:, :-(-T // 128)].all(1)  # [Hkv][128]
+        range_v = 255.0 * np.asarray(meta.v_scale[b], np.float64)  # [Hkv][tokens]
+        for h in range(c.Hkv):
+            k, v, span = K[:, h], V[:, h], np.repeat(spread[h], 128, 0)[:T]
+            top_k, top_v = np.abs(k).max(0), np.abs(v).max()
+            for i, seen in enumerate(tree.ancestors(parents[b])):
+                if seen is None:
+                    continue
+                x = f64(q[b, i, h * G:(h + 1) * G]) / np.sqrt(D)  # [G][128]
+                keys, values = np.concatenate([k, f64(kn[b, seen, h])]), np.concatenate([v, f64(vn[b, seen, h])])
+                s = x @ keys.T
+                p = np.exp(s - s.max(1, keepdims=True))
+                d = 2.0 ** -21 * (np.abs(x) @ np.abs(keys).T)
+                d[:, :T] += 2.0 ** -12 * (np.abs(x) @ np.where(around[h], np.minimum(np.abs(k), span), span).T)
+                if wide == 0:
+                    d[:, :T] += 2.0 ** -21 * (np.abs(x) @ span.T)
+                d += 2.0 ** -39 * (np.abs(x) @ top_k + 128 * (np.abs(x) * top_k).max(1))[:, None]
+                floor = np.minimum(p, 2.0 ** -33) / p.sum(1, keepdims=True)
+                p /= p.sum(1, keepdims=True)
+                o = p @ values
+                # (only tokens that have weight set the largest error that counts; the others' weights
+                # stay below a millionth of it even e^2d times as large)
+                heavy = p > 1e-9 * p.max(1, keepdims=True)
+                worst = np.where(heavy, d, 0).max(1)
+                off = (p * (worst * np.exp(2 * worst) + 2.0 ** -12)[:, None] + floor)
+                for g in range(G):
+                    dev = np.abs(values - o[g])
+                    t = off[g] @ dev + 2.0 ** -12 * (p[g] @ np.abs(values)) + 2.0 ** -39 * top_v + 2.0 ** -8 * np.abs(o[g])
+                    if wide == 0:
+                        t += 2.0 ** -11 * (p[g, :T] @ range_v[h, :T])
+                    out[b, i, h * G + g], tol[b, i, h * G + g] = o[g], t
+    return out, tol
+
+
+def check(c, q, kn, vn, wide, parents):
+    want, tol = reference(c, q, kn, vn, parents, wide)
+    got = run(c, q, kn, vn, parents, wide=wide).astype(np.float64)
+    assert np.isfinite(got).all()
+    err = np.abs(got - want)
+    at = np.unravel_index(np.argmax(err - tol), err.shape)
+    print(f"largest error {err.max():.2e}, of its tolerance at most {np.max(err / (tol + 1e-300)):.2f}")
+    assert (err <= tol).all(), (at, got[at], want[at], tol[at], int((err > tol).sum()))
+
+
+def made(lens, Hkv, change, bt=16, Hq=None, n=30):
+    """A cache of N(0, 1) keys and values, queries and nodes, after change(k, v, q) of
+    the fp32 inputs (k, v: [T][Hkv][128]; q: [n][Hq][128] of the sequence)."""
+    Hq = Hq or 4 * Hkv
+    ks, vs, qs = [], [], []
+    for b, T in enumerate(lens):
+        k, v = (x.float() for x in random_kv(T, Hkv, seed=40 + b, outlier_cols=0))
+        q = random_bf16((n, Hq, 128), 70 + b).float()
+        change(k, v, q)
+        ks.append(k.bfloat16()), vs.append(v.bfloat16()), qs.append(q.bfloat16())
+    c = build_cache(ks, vs, Hkv, bt=bt, with_oracle=False)
+    B = len(lens)
+    return c, torch.stack(qs), random_bf16((B, n, Hkv, 128), 5), random_bf16((B, n, Hkv, 128), 6)
+
+
+@pytest.mark.parametrize("power,wide", [(8, 0), (12, 1), (20, 1), (27, 1), (20, 2), (27, 2)])
+def test_a_token_of_large_values_and_no_weight(power, wide):
+    def change(k, v, q):
+        v[77] *= 2.0 ** power
+        k[77] = -3.0 * torch.sign(q[0, 0])  # far below the others for queries of these signs
+        q[:] = torch.abs(q) * torch.sign(q[0, 0])
+    c, *x = made([1500, 333], 2, change)
+    check(c, *x, wide, random_parents(2, 30, seed=4))
