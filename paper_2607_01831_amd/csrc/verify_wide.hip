@@ -24,9 +24,10 @@
 //    |V|, rounded to fp16: off by 2^-12 of itself, and by 2^-40 of the largest where
 //    it is a subnormal (the largest stands at fp16's upper end, 2^15, so that one
 //    token's large values leave the others their bits).
-//  * weights p <= 2^8 against a reference that follows the row's maximum once it is
-//    2^8 behind, rounded to 11 bits; l sums the rounded weights, so that an output is
-//    a mean by them, in fp32.
+//  * weights 2^8 p against a reference that follows the row's maximum once it is 2^7
+//    behind, so up to 2^15, rounded to fp16: off by 2^-12 of themselves, or by 2^-33 of
+//    the row's largest; l sums the rounded weights, so that an output is a mean by
+//    them, in fp32.
 //
 // A step is a tile of 32 tokens for 256 rows, or, for half the rows, two tiles
 // with a wavefront's two partners each on one (TS 2; they join at the end).  A
@@ -68,8 +69,9 @@ constexpr int kRawBytes = kRawMeta + 2 * kTile * 4;
 constexpr int kFragBytes = 8 * 1024;                // a tile's 8 fragments of K, or of V
 constexpr int kFragsV = 3;                          // V's buffers; K's are two
 constexpr int kDepth = 4;                           // steps whose copies are in flight or not converted yet
-constexpr float kSlack = 8.0f;                      // log2 units that the reference may lag behind
 constexpr int kUpper = 15;                          // fp16 operands reach up to 2^15
+constexpr float kSlack = 7.0f;                      // log2 units that the reference may lag behind
+constexpr float kLift = kUpper - kSlack;            // ... that weights are held above it
 
 // TS: tiles of a step, one for each TS-th of the wavefronts.
 template <int LAYOUT, int TS>
@@ -238,7 +240,7 @@ __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<
 #pragma unroll
         for (int i = 1; i < kWaves; ++i) v = fmax2(v, s_vmax[i]);
         if (v > 0.0f && v <= FLT_MAX) frexpf(v, &Ev);
-        Ev = min(max(Ev, kUpper - 126), 126);  // 2^(Ev - kUpper) and its inverse are normal numbers
+        Ev = min(max(Ev, kUpper + (int)kLift - 126), 126);  // 2^(Ev - kUpper - kLift) is a normal number
     }
     __syncthreads();
 
@@ -349,9 +351,9 @@ __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<
     load_group(0);
     for (int j = 0; j < min(n_steps, 2); ++j)
         for (int k = 0; k < TS; ++k) convert(j, k, load_raw(j, k));
-    // the reference (-FLT_MAX while no token has been seen: a number, so that -inf
-    // less it is -inf), and where it follows
-    float m_run[2] = {-FLT_MAX, -FLT_MAX}, follow[2] = {-FLT_MAX, -FLT_MAX};
+    // what is added to a score: kLift less the reference (FLT_MAX while no token has
+    // been seen: a number, so that -inf and it are -inf)
+    float lift[2] = {FLT_MAX, FLT_MAX};
     f32x4_t acc[2][8], l[2] = {};  // l: the sums of the weights, a ninth column of the values, all ones
     const u32x4_t ones = {0x3C003C00u, 0x3C003C00u, 0x3C003C00u, 0x3C003C00u};
 #pragma unroll
@@ -404,13 +406,12 @@ __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<
             const f32x4_t &x = s[rt][0], &y = s[rt][1];
             top[rt] = fmax3(fmax3(x[0], x[1], x[2]), fmax3(x[3], y[0], y[1]), fmax2(y[2], y[3])) * sc[rt];
         }
-        if (__any(top[0] > follow[0] || top[1] > follow[1])) {
+        if (__any(top[0] + lift[0] > kUpper || top[1] + lift[1] > kUpper)) {
 #pragma unroll
             for (int rt = 0; rt < 2; ++rt) {
-                const float m = fmaxf(max_kg(top[rt]), m_run[rt]);
-                const float alpha = __builtin_amdgcn_exp2f(m_run[rt] - m);
-                m_run[rt] = m;
-                follow[rt] = m + kSlack;
+                const float next = fminf(kLift - max_kg(top[rt]), lift[rt]);
+                const float alpha = __builtin_amdgcn_exp2f(next - lift[rt]);
+                lift[rt] = next;
                 float af[4];
 #pragma unroll
                 for (int i = 0; i < 4; ++i) af[i] = __shfl(alpha, 4 * kg + i);
@@ -435,7 +436,7 @@ __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<
             const f32x4_t &x = s[rt][0], &y = s[rt][1];
             float p[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(i < 4 ? x[i & 3] : y[i & 3], sc[rt], -m_run[rt]));
+            for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(i < 4 ? x[i & 3] : y[i & 3], sc[rt], lift[rt]));
 #pragma unroll
             for (int e = 0; e < 4; ++e) pa[rt][e] = pack_f16_rne(p[2 * e], p[2 * e + 1]);
         }
@@ -483,22 +484,23 @@ __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<
 
     // ---- the partials ----
     const bool any_bad = __syncthreads_or(bad);
-    const float up = ldexpf(1.0f, Ev - kUpper);
+    const float up = ldexpf(1.0f, Ev - kUpper - (int)kLift);
     // Of row tile rt, through LDS, so that rows are written whole: 8 rows of the
     // wavefront at a time.
     float *s_o = reinterpret_cast<float *>(&s_frag[0][0][0]) + (size_t)w * 8 * (kHeadDim + 4);
     static_assert(kWaves * 8 * (kHeadDim + 4) * 4 <= (2 + kFragsV) * kFragBytes, "the rows must fit in the operands' place");
-    auto write_tile = [&](int rt, float m, f32x4_t l4, const f32x4_t (&o)[8]) {
+    auto write_tile = [&](int rt, float lift_rt, f32x4_t l4, const f32x4_t (&o)[8]) {
         float sum = 0.0f;  // of row col: element col % 4 of the lanes of kg = col / 4
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
             const float x = __shfl(l4[i], 16 * (col >> 2));
             sum = (col & 3) == i ? x : sum;
         }
+        sum *= 1.0f / (1 << (int)kLift);
         if (any_bad) sum = NAN;
         const int r = row0 + 16 * rt + col;
         if (kg == 0 && r < a.rows_total) {
-            const f32x2_t ml = {m == -FLT_MAX ? -INFINITY : m, sum};
+            const f32x2_t ml = {lift_rt == FLT_MAX ? -INFINITY : kLift - lift_rt, sum};
             __builtin_nontemporal_store(ml, reinterpret_cast<f32x2_t *>(a.ws_ml + partial_index(r)));
         }
 #pragma unroll
@@ -526,8 +528,8 @@ __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<
     };
     if constexpr (TS == 1) {
         if (!rows_live) return;
-        write_tile(0, m_run[0], l[0], acc[0]);
-        write_tile(1, m_run[1], l[1], acc[1]);
+        write_tile(0, lift[0], l[0], acc[0]);
+        write_tile(1, lift[1], l[1], acc[1]);
     } else {
         // Two wavefronts have the same rows: each gives the other what it has of
         // one row tile (ts 0 of tile 1, ts 1 of tile 0) and writes the other tile.
@@ -538,12 +540,12 @@ __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<
 #pragma unroll
         for (int c = 0; c < 8; ++c) s_x[(w * 9 + c) * 64 + lane] = one ? acc[0][c] : acc[1][c];
         s_x[(w * 9 + 8) * 64 + lane] = one ? l[0] : l[1];
-        s_y[w * 64 + lane] = one ? m_run[0] : m_run[1];
+        s_y[w * 64 + lane] = one ? lift[0] : lift[1];
         __syncthreads();
         const int other = w ^ (kWaves / TS);
-        const float m_other = s_y[other * 64 + lane];
-        const float m_own = one ? m_run[1] : m_run[0], m = fmaxf(m_own, m_other);
-        const float f_own = __builtin_amdgcn_exp2f(m_own - m), f = __builtin_amdgcn_exp2f(m_other - m);
+        const float lift_other = s_y[other * 64 + lane];
+        const float lift_own = one ? lift[1] : lift[0], lift_rt = fminf(lift_own, lift_other);
+        const float f_own = __builtin_amdgcn_exp2f(lift_rt - lift_own), f = __builtin_amdgcn_exp2f(lift_rt - lift_other);
         float fo[4], ft[4];
 #pragma unroll
         for (int i = 0; i < 4; ++i) {
@@ -559,7 +561,7 @@ __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<
             for (int i = 0; i < 4; ++i) o[c][i] = fmaf(x[i], ft[i], y[i] * fo[i]);
         }
         __syncthreads();  // the exchange is read
-        if (rows_live) write_tile(ts, m, o[8], reinterpret_cast<const f32x4_t(&)[8]>(o));
+        if (rows_live) write_tile(ts, lift_rt, o[8], reinterpret_cast<const f32x4_t(&)[8]>(o));
     }
 }
 

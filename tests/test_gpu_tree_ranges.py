@@ -111,3 +111,27 @@ def test_a_token_of_large_values_and_no_weight(power, wide):
         q[:] = torch.abs(q) * torch.sign(q[0, 0])
     c, *x = made([1500, 333], 2, change)
     check(c, *x, wide, random_parents(2, 30, seed=4))
+
+
+def tail(k, v, q, drop):
+    k[:] = 0
+    k[5, :, 0] = drop * np.sqrt(128) / 128
+    q[:] = 0
+    q[..., 0] = 128
+    v[:] = torch.where(torch.arange(128) % 2 == 0, 1.0, 0.5)
+    v[5] = 0
+
+
+@pytest.mark.parametrize("wide", [1, 2])
+@pytest.mark.parametrize("drop", [16.5, 17.5, 18.2])
+def test_a_long_tail_of_small_weights(drop, wide):
+    """One token e^drop times as heavy as every other, whose values are 0: an output is
+    the tail's sum, and a kernel that drops weights of 2^-25 (e^-17.3) drops it."""
+    c, q, kn, vn = made([16384, 9000], 8, lambda k, v, q: tail(k, v, q, drop), bt=None, Hq=24)
+    kn[..., 0] = -4.0  # the nodes have no weight (e^-45), so that all rows are the first node's
+    parents = np.full((2, 30), -1, np.int32)
+    want, tol = reference(c, q[:, :1], kn[:, :1], vn[:, :1], parents[:, :1], wide)
+    assert (tol < 0.03 * np.abs(want) + 1e-9).all()  # (the rounding of the weights 1 %, of the dominant score 1, of the output 0.4)
+    err = np.abs(run(c, q, kn, vn, parents, wide=wide) - want)
+    print(f"largest error {err.max():.2e}, of its tolerance at most {np.max(err / tol):.2f}")
+    assert (err <= tol).all(), (err.max(), int((err > tol).sum()))
