@@ -536,6 +536,13 @@ int lynx_hkv_dequant(const lynx_layout *L, int32_t b, int32_t T, const int32_t *
  *   lynx_attn_workspace_bytes(L, B, Hq, n, max_seq_len)
  * A node's K and V reach the rows of its descendants and its own alone,
  * whatever they hold (NaN and infinities included).
+ * Precision: with up to 64 rows a kv head (n Hq / num_kv_heads), and with more
+ * over short contexts, the context is attended as by lynx_attn_verify: there a
+ * token's values lose bits where its V scale is 2^13 times smaller than the
+ * largest of the context.  Otherwise a key is off by at most 2^-12 of the range
+ * of its K group, a value by 2^-12 of itself (2^-40 of the largest), a weight by
+ * 2^-12 of itself (2^-33 of the row's largest).  The choice goes by B, n and
+ * max_seq_len, which is best near the lengths.
  */
 int lynx_attn_verify_tree(const lynx_layout *L, int32_t B, int32_t Hq, int32_t n,
                           int32_t max_seq_len, const int32_t *seq_lens, const int32_t *block_table,

@@ -11,15 +11,18 @@
 // order in LDS, and the queries are converted once.
 //
 // Operands:
-//  * K' = (zero + code scale) 2^-e_d, e_d the exponent of the largest |K| of
-//    channel d in the segment (from the metadata), so |K'| <= 1; the query is
-//    q_d 2^(e_d - E), E the exponent of the row's largest product: exact in fp16
-//    (BF16 has 8 significant bits) down to 2^-17 of the largest.  K' is computed in
-//    fp16 as (code - 128) scale' + centre', scale', centre' = zero' + 128 scale' and
-//    the result each rounded to 11 bits: off by at most 2^-12 (|K' - centre'| +
-//    |centre'| + |K'|), where the BF16 key was off by 2^-9 |K'| to begin with.  128
-//    such errors are independent: a score moves by some 2e-4 of the root mean
-//    square of its terms times sqrt(128).
+//  * K' = (zero + code scale - c) 2^(15 - e_d), e_d the exponent of the largest |K| of
+//    channel d in the segment (from the metadata), c a number inside the range of the
+//    group: 0 at first, and from group to group moved to the range's end where it is
+//    outside.  K' is computed in fp32 and rounded to fp16 once: a key is off by 2^-12
+//    of its group's range at most, a sixteenth of a code's step (of itself where c is
+//    0; and by 2^-40 of the channel's largest where it is a subnormal).  So neither
+//    what the keys of a group have in common, which the softmax does not see, nor a
+//    token far from the others takes bits from the rest.  sum_d q_d c_d, of exact
+//    products (c has fp16's 11 bits), is added to the scores in fp32, where they
+//    become weights; it is computed again where a c has moved (each time: 3 % more).
+//  * the query is q_d 2^(e_d - E + 15), E the exponent of the row's largest product:
+//    exact in fp16 (BF16 has 8 significant bits) down to 2^-32 of the largest.
 //  * V' = (zero + code scale) 2^(15 - Ev), Ev the exponent of the segment's largest
 //    |V|, rounded to fp16: off by 2^-12 of itself, and by 2^-40 of the largest where
 //    it is a subnormal (the largest stands at fp16's upper end, 2^15, so that one
@@ -56,16 +59,14 @@
 namespace lynx {
 namespace {
 
-typedef _Float16 h2 __attribute__((ext_vector_type(2)));
-
 constexpr int kWaves = 8;
 constexpr int kThreads = 64 * kWaves;
 static_assert(kWideRows == 32 * kWaves, "two row tiles per wavefront");
 constexpr int kTile = 32;  // tokens
 constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kRawPlane = kTile * kCodeRow;         // 4 KB of codes
-constexpr int kRawMeta = 2 * kRawPlane;             // V scale[32] | V zero[32]
-constexpr int kRawBytes = kRawMeta + 2 * kTile * 4;
+constexpr int kRawBytes = 2 * kRawPlane;
+constexpr int kMetaSlots = 8;                       // steps that V metadata is kept of
 constexpr int kFragBytes = 8 * 1024;                // a tile's 8 fragments of K, or of V
 constexpr int kFragsV = 3;                          // V's buffers; K's are two
 constexpr int kDepth = 4;                           // steps whose copies are in flight or not converted yet
@@ -97,9 +98,14 @@ __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<
 
     __shared__ __attribute__((aligned(16))) uint8_t s_raw[kDepth][TS][kRawBytes];
     __shared__ __attribute__((aligned(16))) uint8_t s_frag[2 + kFragsV][TS][kFragBytes];
-    __shared__ __attribute__((aligned(16))) float s_km[2][2 * kHeadDim];  // K scale | zero of a group, two groups
+    __shared__ __attribute__((aligned(16))) float s_vm[kMetaSlots][TS][2 * kTile];  // a tile's V scale | zero
+    __shared__ __attribute__((aligned(16))) float s_km[3][2 * kHeadDim];  // K scale | zero of a group, three groups
     __shared__ int32_t s_ids[LAYOUT == 0 ? 1 : kWaves][2 * kDepth][TS][8];  // blocks of a step's rows
     __shared__ int s_e[kHeadDim];                                       // channel exponents
+    // of two groups: scale and zero - c of the conversion, and c
+    __shared__ __attribute__((aligned(16))) float s_kp[2][2][kHeadDim];
+    __shared__ __attribute__((aligned(16))) _Float16 s_c[2][kHeadDim];
+    __shared__ __attribute__((aligned(8))) int s_moved[2][2];  // by half the channels
     __shared__ float s_vmax[kWaves];
     float(*s_max)[kHeadDim] = reinterpret_cast<float(*)[kHeadDim]>(&s_frag[0][0][0]);  // (before there are fragments)
     auto frag_k = [&](int j) { return s_frag[j & 1]; };
@@ -119,8 +125,8 @@ __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<
     const uint32_t block_rows = (uint32_t)Hkv * a.geo.bt, head_rows = (uint32_t)h * a.geo.bt;
     auto token_of = [&](int j, int k) { return min(first + kTile * (TS * j + k) + 8 * (w & 3) + crow, T - 1); };
     // Every wavefront issues as many operations per step, so that it can wait for
-    // the older ones: for each tile a copy of rows, one of metadata (K's with a
-    // group's first step, by wavefront TS; else V's of tile w % TS, which may be
+    // the older ones: for each tile a copy of rows, one of metadata (of the next step:
+    // K's where a group begins, by wavefront TS; else V's of tile w % TS, which may be
     // written more than once), and the block numbers of a later step.
     // Wavefront w copies rows 8 (w % 4) .. + 7 of K (w < 4) or V.
     constexpr int kOps = TS + (LAYOUT == 0 ? 1 : 2);
@@ -138,6 +144,14 @@ __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<
     const uint32_t km0 = lds_addr(&s_km[0][0]);
     const uint32_t raw0 = lds_addr(&s_raw[0][0][0]);
     auto raw_of = [&](int j, int k) { return raw0 + (uint32_t)((j % kDepth) * TS + k) * kRawBytes; };
+    auto copy_km = [&](int g) {
+        lds_copy16((lane < 32 ? a.meta.k_scale : a.meta.k_zero) + kmeta + (size_t)(g0 + g) * kHeadDim + 4 * (lane & 31),
+                   km0 + (uint32_t)(g % 3) * 2 * kHeadDim * 4);
+    };
+    auto copy_vm = [&](int j) {
+        const int tt = min(first + kTile * (TS * j + w % TS) + (lane & 31), T - 1);
+        lds_copy4((lane < 32 ? a.meta.v_scale : a.meta.v_zero) + vmeta + tt, lds_addr(&s_vm[j % kMetaSlots][w % TS][0]));
+    };
     auto issue = [&](int j, auto id_of) {
         if (j >= n_steps) return;
 #pragma unroll
@@ -158,14 +172,10 @@ __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<
             lds_copy16(codes + (size_t)((uint32_t)id * block_rows + head_rows + place_in(t)) * kCodeRow + chunk_off,
                        raw_of(j, k) + 1024u * w);
         }
-        if (w == TS && j % kSteps == 0) {
-            const int g = j / kSteps;
-            lds_copy16((lane < 32 ? a.meta.k_scale : a.meta.k_zero) + kmeta + (size_t)(g0 + g) * kHeadDim + 4 * (lane & 31),
-                       km0 + (uint32_t)(g & 1) * 2 * kHeadDim * 4);
-        } else {
-            const int tt = min(first + kTile * (TS * j + w % TS) + (lane & 31), T - 1);
-            lds_copy4((lane < 32 ? a.meta.v_scale : a.meta.v_zero) + vmeta + tt, raw_of(j, w % TS) + kRawMeta);
-        }
+        if (w == TS && (j + 1) % kSteps == 0 && j + 1 < n_steps)
+            copy_km((j + 1) / kSteps);
+        else
+            copy_vm(j + 1);
         copy_ids(j + kDepth);
     };
 
@@ -178,6 +188,8 @@ __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<
             for (int k = 0; k < TS; ++k) ids[j][k] = LAYOUT == 0 ? 0 : bt_row[block_of(token_of(j, k))];
 #pragma unroll
         for (int j = 0; j < kDepth; ++j) issue(j, [&](int k) { return ids[j][k]; });
+        if (w == TS) copy_km(0);
+        copy_vm(0);
     }
     // the wavefront's queries: row col of each row tile, dims 8 kg + 32 kk
     uint4 qraw[2][4];
@@ -277,11 +289,12 @@ __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const int d = 32 * kk + 8 * kg + 2 * e;
-                qf[rt][kk][e] = pack_f16_rne(ldexpf(bf16_lo(x[kk][e]), s_e[d] - E), ldexpf(bf16_hi(x[kk][e]), s_e[d + 1] - E));
+                qf[rt][kk][e] = pack_f16_rne(ldexpf(bf16_lo(x[kk][e]), s_e[d] - E + kUpper),
+                                             ldexpf(bf16_hi(x[kk][e]), s_e[d + 1] - E + kUpper));
             }
         // positive and finite: times the -inf of a token past the context it must
         // not be a NaN
-        sc[rt] = __builtin_amdgcn_fmed3f(ldexpf(kLog2e * rsqrtf((float)kHeadDim), E), FLT_MIN, FLT_MAX);
+        sc[rt] = __builtin_amdgcn_fmed3f(ldexpf(kLog2e * rsqrtf((float)kHeadDim), E - 2 * kUpper), FLT_MIN, FLT_MAX);
     }
 
     // ---- conversion of a step into operand order ----
@@ -289,29 +302,48 @@ __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<
     // fragment c: lane (dim 16 c + col, tokens 16 (e / 4) + 4 kg + e % 4).  Wavefront
     // w makes fragment w of each.
     const int kk_own = w & 3;
-    h2 ks[4], kz[4];
-    auto load_group = [&](int j) {
+    auto prepare = [&](int g) {  // a thread per channel
+        if (w >= kHeadDim / 64) return;
+        const float *km = s_km[g % 3];
+        const int up = kUpper - s_e[tid];
+        const float scale = ldexpf(km[tid], up), zero = ldexpf(km[kHeadDim + tid], up);
+        const float was = g > 0 ? (float)s_c[~g & 1][tid] : 0.0f;
+        const _Float16 c = (_Float16)__builtin_amdgcn_fmed3f(was, zero, fmaf(255.0f, scale, zero));
+        const bool moved = __any((float)c != was);
+        if (lane == 0) s_moved[g & 1][w] = moved;
+        s_kp[g & 1][0][tid] = scale;
+        s_kp[g & 1][1][tid] = zero - (float)c;
+        s_c[g & 1][tid] = c;
+    };
+    // The queries' products with the c of step j's group, as those with a tile whose
+    // tokens are all c: what its scores are off by, times their scale.
+    float off[2] = {0.0f, 0.0f};
+    auto load_off = [&](int j) {
+        f32x4_t x[2] = {};
 #pragma unroll
-        for (int e = 0; e < 8; ++e) {
-            const int d = 32 * kk_own + 8 * kg + e;
-            const float *km = s_km[(j / kSteps) & 1];
-            const float sc = ldexpf(km[d], -s_e[d]);
-            ks[e / 2][e % 2] = (_Float16)sc;
-            kz[e / 2][e % 2] = (_Float16)fmaf(128.0f, sc, ldexpf(km[kHeadDim + d], -s_e[d]));
+        for (int kk = 0; kk < 4; ++kk) {
+            const u32x4_t c = *reinterpret_cast<const u32x4_t *>(&s_c[(j / kSteps) & 1][32 * kk + 8 * kg]);
+#pragma unroll
+            for (int rt = 0; rt < 2; ++rt) x[rt] = mfma_f16(c, qf[rt][kk], x[rt]);
         }
+#pragma unroll
+        for (int rt = 0; rt < 2; ++rt) off[rt] = x[rt][0] * sc[rt];
     };
     const float down = ldexpf(1.0f, kUpper - Ev);
+    auto prepare_v = [&](int j) {
+        if (w < TS) s_vm[j % kMetaSlots][w][lane] *= down;
+    };
     // (of a step past the last: what its slot holds, to where nothing reads)
     struct Raw {
         uint2 k;
         intx2_t v;
-        float4 s[2], z[2];
+        float4 s[2], z[2], ks[2], kz[2];
     };
     auto load_raw = [&](int j, int k) {
         const int t = 16 * (w >> 2) + col, q = 2 * kk_own + (kg >> 1);
         const int tr = 16 * ((col >> 1) >> 2) + 4 * kg + ((col >> 1) & 3);
         const uint8_t *p = s_raw[j % kDepth][k];
-        const float *vm = reinterpret_cast<const float *>(p + kRawMeta) + 4 * kg;
+        const float *vm = &s_vm[j % kMetaSlots][k][4 * kg];
         Raw r;
         r.k = *reinterpret_cast<const uint2 *>(p + t * kCodeRow + ((q ^ (t & 7)) * 16) + 8 * (kg & 1));
         r.v = __builtin_amdgcn_ds_read_tr8_b64_v2i32(
@@ -320,18 +352,21 @@ __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<
         for (int i = 0; i < 2; ++i) {
             r.s[i] = *reinterpret_cast<const float4 *>(vm + 16 * i);
             r.z[i] = *reinterpret_cast<const float4 *>(vm + kTile + 16 * i);
+            const float *kp = &s_kp[(j / kSteps) & 1][0][32 * kk_own + 8 * kg + 4 * i];
+            r.ks[i] = *reinterpret_cast<const float4 *>(kp);
+            r.kz[i] = *reinterpret_cast<const float4 *>(kp + kHeadDim);
         }
         return r;
     };
     auto convert = [&](int j, int k, const Raw &raw) {
         u32x4_t o;
+        const float ks[8] = {raw.ks[0].x, raw.ks[0].y, raw.ks[0].z, raw.ks[0].w, raw.ks[1].x, raw.ks[1].y, raw.ks[1].z, raw.ks[1].w};
+        const float kz[8] = {raw.kz[0].x, raw.kz[0].y, raw.kz[0].z, raw.kz[0].w, raw.kz[1].x, raw.kz[1].y, raw.kz[1].z, raw.kz[1].w};
 #pragma unroll
         for (int e = 0; e < 4; ++e) {
-            // a byte under 0x64 is 1024 + code
-            const uint32_t code =
-                __builtin_amdgcn_perm(0x64646464u, e < 2 ? raw.k.x : raw.k.y, e & 1 ? 0x04030402u : 0x04010400u);
-            const h2 x = __builtin_bit_cast(h2, code) - (h2){(_Float16)1152.0f, (_Float16)1152.0f};
-            o[e] = __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(x, ks[e], kz[e]));
+            const uint32_t x = (e < 2 ? raw.k.x : raw.k.y) >> (16 * (e & 1));
+            o[e] = pack_f16_rne(fmaf((float)(x & 0xFFu), ks[2 * e], kz[2 * e]),
+                                fmaf((float)((x >> 8) & 0xFFu), ks[2 * e + 1], kz[2 * e + 1]));
         }
         *reinterpret_cast<u32x4_t *>(frag_k(j)[k] + w * 1024 + 16 * lane) = o;
         const float4 *s = raw.s, *z = raw.z;
@@ -340,15 +375,17 @@ __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<
 #pragma unroll
         for (int e = 0; e < 8; e += 2) {
             const uint32_t x = (uint32_t)raw.v[e >> 2] >> (8 * (e & 3));
-            o[e / 2] = pack_f16_rne(down * fmaf((float)(x & 0xFFu), vs[e], vz[e]),
-                                    down * fmaf((float)((x >> 8) & 0xFFu), vs[e + 1], vz[e + 1]));
+            o[e / 2] = pack_f16_rne(fmaf((float)(x & 0xFFu), vs[e], vz[e]), fmaf((float)((x >> 8) & 0xFFu), vs[e + 1], vz[e + 1]));
         }
         *reinterpret_cast<u32x4_t *>(frag_v(j)[k] + w * 1024 + 16 * lane) = o;
     };
 
     wait_vmcnt<0>();
     __syncthreads();
-    load_group(0);
+    prepare(0);
+    if (kSteps == 2) prepare(1);  // (step 2's, which iteration 0 converts)
+    for (int j = 0; j < 3; ++j) prepare_v(j);
+    __syncthreads();
     for (int j = 0; j < min(n_steps, 2); ++j)
         for (int k = 0; k < TS; ++k) convert(j, k, load_raw(j, k));
     // what is added to a score: kLift less the reference (FLT_MAX while no token has
@@ -388,7 +425,12 @@ __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<
         issue(j + kDepth, [&](int k) {
             return LAYOUT == 0 ? 0 : s_ids[LAYOUT == 0 ? 0 : w][(j + kDepth) % (2 * kDepth)][k][crow];
         });
-        if ((j + 2) % kSteps == 0) load_group(j + 2);
+        if ((j + 3) % kSteps == 0) prepare((j + 3) / kSteps);
+        prepare_v(j + 3);
+        if (j % kSteps == 0) {
+            const int2 moved = *reinterpret_cast<const int2 *>(s_moved[(j / kSteps) & 1]);
+            if (__builtin_amdgcn_readfirstlane(moved.x | moved.y)) load_off(j);
+        }
         const int t0 = first + kTile * (TS * j + ts);
         if (t0 + kTile > end) {
 #pragma unroll
@@ -404,7 +446,7 @@ __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<
 #pragma unroll
         for (int rt = 0; rt < 2; ++rt) {
             const f32x4_t &x = s[rt][0], &y = s[rt][1];
-            top[rt] = fmax3(fmax3(x[0], x[1], x[2]), fmax3(x[3], y[0], y[1]), fmax2(y[2], y[3])) * sc[rt];
+            top[rt] = fmaf(fmax3(fmax3(x[0], x[1], x[2]), fmax3(x[3], y[0], y[1]), fmax2(y[2], y[3])), sc[rt], off[rt]);
         }
         if (__any(top[0] + lift[0] > kUpper || top[1] + lift[1] > kUpper)) {
 #pragma unroll
@@ -434,9 +476,10 @@ __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<
 #pragma unroll
         for (int rt = 0; rt < 2; ++rt) {
             const f32x4_t &x = s[rt][0], &y = s[rt][1];
+            const float c0 = off[rt] + lift[rt];
             float p[8];
 #pragma unroll
-            for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(i < 4 ? x[i & 3] : y[i & 3], sc[rt], lift[rt]));
+            for (int i = 0; i < 8; ++i) p[i] = __builtin_amdgcn_exp2f(fmaf(i < 4 ? x[i & 3] : y[i & 3], sc[rt], c0));
 #pragma unroll
             for (int e = 0; e < 4; ++e) pa[rt][e] = pack_f16_rne(p[2 * e], p[2 * e + 1]);
         }
@@ -459,7 +502,7 @@ __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<
 #pragma unroll
                 for (int rt = 0; rt < 2; ++rt) l[rt] = mfma_f16(pa[rt], ones, l[rt]);
             convert(j + 2, k, raw);
-            __builtin_amdgcn_sched_group_barrier(0x100, 6, 1);
+            __builtin_amdgcn_sched_group_barrier(0x100, 10, 1);
             constexpr int kFirst = 4;  // products that run while the codes come in
             __builtin_amdgcn_sched_group_barrier(0x8, kFirst, 1);
 #pragma unroll

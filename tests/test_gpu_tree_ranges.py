@@ -135,3 +135,62 @@ def test_a_long_tail_of_small_weights(drop, wide):
     err = np.abs(run(c, q, kn, vn, parents, wide=wide) - want)
     print(f"largest error {err.max():.2e}, of its tolerance at most {np.max(err / tol):.2f}")
     assert (err <= tol).all(), (err.max(), int((err > tol).sum()))
+
+
+def offset(k, v, q, mean, query):
+    """Two channels whose keys have a mean that the softmax does not see."""
+    k[:, :, [3, 9]] += mean
+    q[..., 3] += query
+    q[..., 9] -= query
+
+
+@pytest.mark.parametrize("wide", [0, 1, 2])
+@pytest.mark.parametrize("mean,query", [(30, 10), (50, 20), (64, 32), (-100, 30), (1000, 10)])
+def test_keys_far_from_zero(mean, query, wide):
+    c, *x = made([1500, 333], 2, lambda k, v, q: offset(k, v, q, mean, query))
+    check(c, *x, wide, random_parents(2, 30, seed=4))
+
+
+def moving(k, v, q):
+    """The mean changes from group to group, and some groups are one value."""
+    offset(k, v, q, 0, 20)
+    for g in range(-(-len(k) // 128)):
+        k[128 * g:128 * g + 128, :, [3, 9]] += (0, 50, -70, 200)[g % 4]
+    k[256:384] = 0
+    k[640:768, :, 9] = 33.0
+
+
+@pytest.mark.parametrize("wide", [0, 1, 2])
+def test_keys_whose_mean_moves(wide):
+    c, *x = made([1500, 900], 2, moving)
+    check(c, *x, wide, random_parents(2, 30, seed=4))
+
+
+def far_token(k, v, q, power, at):
+    """A token 2^power times as large as the others, against every query's signs."""
+    k[at] *= 2.0 ** power
+    sign = torch.sign(q[0, :1])
+    q[:] = torch.abs(q) * sign
+    k[at] = -torch.abs(k[at]) * sign
+
+
+@pytest.mark.parametrize("at", [77, 200])
+@pytest.mark.parametrize("power,wide", [(9, 0), (10, 0), (9, 1), (10, 1), (20, 1), (9, 2), (10, 2), (20, 2)])
+def test_a_token_far_from_the_others(power, at, wide):
+    c, *x = made([1500, 333], 2, lambda k, v, q: far_token(k, v, q, power, at))
+    check(c, *x, wide, random_parents(2, 30, seed=4))
+
+
+def small_groups(k, v, q):
+    """Groups a thousand and a million times smaller than the others, with queries that
+    see no more of the larger ones than of them."""
+    k[128:256, :, 64:] *= 2.0 ** -10
+    k[:, :, :4] *= 2.0 ** 20
+    k[256:384, :, :4] *= 2.0 ** -20
+    q[..., :4] *= 2.0 ** -20
+
+
+@pytest.mark.parametrize("wide", [0, 1, 2])
+def test_groups_of_other_sizes(wide):
+    c, *x = made([1500, 333], 2, small_groups)
+    check(c, *x, wide, random_parents(2, 30, seed=4))
