@@ -385,6 +385,17 @@ def lynx_attn_anchor_decode_tail(L: Layout, B: int, Hq: int, max_seq_len: int, s
         _arg(fn, "lse", lse, B * Hq * 4), _ptr(ws), 0 if ws is None else ws.nbytes, _stream(stream)))
 
 
+def _scratch(make, nbytes: int, device, stream) -> torch.Tensor:
+    """A call's own workspace, made (torch.empty, torch.zeros) on the stream that the
+    call runs on: cleared before it, and free again behind it."""
+    if stream is None:
+        return make(nbytes, dtype=torch.uint8, device=device)
+    if not isinstance(stream, torch.cuda.Stream):
+        stream = torch.cuda.ExternalStream(stream, device) if stream else torch.cuda.default_stream(device)
+    with torch.cuda.stream(stream):
+        return make(nbytes, dtype=torch.uint8, device=device)
+
+
 def lynx_spec_accept_workspace_bytes(B: int, k: int, vocab: int) -> int:
     return int(load().lynx_spec_accept_workspace_bytes(B, k, vocab))
 
@@ -393,12 +404,12 @@ def lynx_spec_accept_greedy(target_logits, draft_tokens, accepted, next_token,
                             workspace_buf=None, stream=None) -> None:
     """target_logits fp32 [B][k+1][V], draft_tokens int32 [B][k]; writes
     accepted and next_token (int32 [B]).  workspace_buf: None allocates
-    lynx_spec_accept_workspace_bytes() bytes with torch."""
+    lynx_spec_accept_workspace_bytes() bytes with torch, on the call's stream."""
     B, k1, V = (int(x) for x in target_logits.shape)
     ws = workspace_buf
     if ws is None:
         n = lynx_spec_accept_workspace_bytes(B, k1 - 1, V)
-        ws = torch.empty(max(n, 16), dtype=torch.uint8, device=target_logits.device)
+        ws = _scratch(torch.empty, max(n, 16), target_logits.device, stream)
     _check("lynx_spec_accept_greedy", load().lynx_spec_accept_greedy(
         B, k1 - 1, V, _ptr(target_logits), _ptr(draft_tokens), _ptr(accepted), _ptr(next_token),
         _ptr(ws), ws.nbytes, _stream(stream)))
@@ -409,12 +420,12 @@ def lynx_spec_accept_sample(target_probs, draft_probs, draft_tokens, uniforms, a
     """target_probs fp32 [B][k+1][V], draft_probs fp32 [B][k][V], draft_tokens
     int32 [B][k], uniforms fp32 [B][k+1]; writes accepted and next_token
     (int32 [B]).  workspace_buf: None allocates
-    lynx_spec_accept_workspace_bytes() bytes with torch."""
+    lynx_spec_accept_workspace_bytes() bytes with torch, on the call's stream."""
     B, k1, V = (int(x) for x in target_probs.shape)
     ws = workspace_buf
     if ws is None:
         n = lynx_spec_accept_workspace_bytes(B, k1 - 1, V)
-        ws = torch.empty(max(n, 16), dtype=torch.uint8, device=target_probs.device)
+        ws = _scratch(torch.empty, max(n, 16), target_probs.device, stream)
     _check("lynx_spec_accept_sample", load().lynx_spec_accept_sample(
         B, k1 - 1, V, _ptr(target_probs), _ptr(draft_probs), _ptr(draft_tokens), _ptr(uniforms),
         _ptr(accepted), _ptr(next_token), _ptr(ws), ws.nbytes, _stream(stream)))
@@ -458,7 +469,11 @@ def lynx_spec_tree_workspace_bytes(B: int, n: int, vocab: int) -> int:
 def spec_tree_workspace(B: int, n: int, vocab: int, device="cuda") -> torch.Tensor:
     """A device buffer of lynx_spec_tree_workspace_bytes() bytes, zero-filled:
     every call finds it zero and leaves it zero."""
-    return torch.zeros(max(lynx_spec_tree_workspace_bytes(B, n, vocab), 16), dtype=torch.uint8, device=device)
+    return _tree_scratch(B, n, vocab, device, None)
+
+
+def _tree_scratch(B: int, n: int, vocab: int, device, stream) -> torch.Tensor:
+    return _scratch(torch.zeros, max(lynx_spec_tree_workspace_bytes(B, n, vocab), 16), device, stream)
 
 
 def _tree_args(fn: str, dev: int, scores, tokens, parents, accepted, path, next_token, uniforms=None):
@@ -478,10 +493,10 @@ def lynx_spec_accept_tree_greedy(target_logits, tokens, parents, accepted, path,
                                  workspace_buf=None, stream=None) -> None:
     """target_logits fp32 [B][n+1][V], tokens and parents int32 [B][n]; writes
     accepted, next_token (int32 [B]) and path (int32 [B][n]).  workspace_buf:
-    spec_tree_workspace(); None makes one for this call."""
-    fn, (dev, stream) = "lynx_spec_accept_tree_greedy", _here(stream)
+    spec_tree_workspace(); None makes one for this call, on its stream."""
+    fn, on, (dev, stream) = "lynx_spec_accept_tree_greedy", stream, _here(stream)
     B, n, V, args = _tree_args(fn, dev, target_logits, tokens, parents, accepted, path, next_token)
-    ws = workspace_buf if workspace_buf is not None else spec_tree_workspace(B, n, V, target_logits.device)
+    ws = workspace_buf if workspace_buf is not None else _tree_scratch(B, n, V, target_logits.device, on)
     _check(fn, load().lynx_spec_accept_tree_greedy(B, n, V, *args, _typed(fn, "workspace_buf", ws, 0, _U8, dev), ws.nbytes,
                                                    stream))
 
@@ -490,11 +505,11 @@ def lynx_spec_accept_tree_sample(target_probs, tokens, parents, uniforms, accept
                                  workspace_buf=None, stream=None) -> None:
     """target_probs fp32 [B][n+1][V], uniforms fp32 [B][n+1]; the rest as
     lynx_spec_accept_tree_greedy."""
-    fn, (dev, stream) = "lynx_spec_accept_tree_sample", _here(stream)
+    fn, on, (dev, stream) = "lynx_spec_accept_tree_sample", stream, _here(stream)
     if uniforms is None:
         raise LynxError(fn, LYNX_EINVAL)
     B, n, V, args = _tree_args(fn, dev, target_probs, tokens, parents, accepted, path, next_token, uniforms)
-    ws = workspace_buf if workspace_buf is not None else spec_tree_workspace(B, n, V, target_probs.device)
+    ws = workspace_buf if workspace_buf is not None else _tree_scratch(B, n, V, target_probs.device, on)
     _check(fn, load().lynx_spec_accept_tree_sample(B, n, V, *args, _typed(fn, "workspace_buf", ws, 0, _U8, dev), ws.nbytes,
                                                    stream))
 
