@@ -9,12 +9,14 @@ from __future__ import annotations
 
 import ctypes
 import struct
+import warnings
 from dataclasses import dataclass
 from pathlib import Path
 
 import torch
 
 LIBRARY = Path(__file__).resolve().parent / "liblynx.so"
+ARGS = LIBRARY.with_name("_args.so")  # host code of the binding
 
 LYNX_OK, LYNX_EINVAL, LYNX_ENOTSUP, LYNX_EWORKSPACE, LYNX_EHIP = 0, -1, -2, -3, -4
 HEAD_DIM = 128
@@ -216,14 +218,23 @@ def _typed_form(fn: str, what: str, t, nbytes: int, dtype, dev: int):
     return t.data_ptr()
 
 
-try:  # the same in C++, which leaves to the form above what does not pass (an
-    # append 9.5 -> 5.7 us on the host)
-    from . import _args
-except ImportError:  # not built
-    _typed = _typed_form
-else:
+def _fastest_typed():
+    """The same in C++, which leaves to the form above what does not pass (an append
+    9.5 -> 5.7 us on the host), or that form where it is not built."""
+    global _args
+    if not ARGS.exists():
+        return _typed_form
+    try:
+        from . import _args
+    except ImportError as e:
+        warnings.warn(f"{ARGS} does not load ({e}): build it again for this Python and torch "
+                      "(python -m paper_2607_01831_amd.build)", RuntimeWarning)
+        return _typed_form
     _args.otherwise(_typed_form)
-    _typed = _args.typed
+    return _args.typed
+
+
+_typed = _fastest_typed()
 
 
 _BF16, _F32, _I32, _U8 = torch.bfloat16, torch.float32, torch.int32, torch.uint8
