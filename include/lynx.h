@@ -522,6 +522,16 @@ int lynx_hkv_dequant(const lynx_layout *L, int32_t b, int32_t T, const int32_t *
  */
 
 /*
+ * lynx_attn_tree_workspace_bytes -- workspace with which lynx_attn_verify_tree has
+ * every kernel to choose from, for `n` nodes per sequence: at least
+ * lynx_attn_workspace_bytes of as many queries (up to four times that from 65 rows
+ * a kv head on), laid out alike, and enough for every smaller call too.  Returns 0
+ * on invalid arguments.
+ */
+size_t lynx_attn_tree_workspace_bytes(const lynx_layout *L, int32_t B, int32_t Hq, int32_t n,
+                                      int32_t max_seq_len);
+
+/*
  * lynx_attn_verify_tree -- the verification pass (Sec. 4.3) over a tree: node
  * i's query attends the whole context (the merged 8-bit cache, zero + code *
  * scale) and, of the nodes, its ancestors and itself, by their own BF16 K/V.
@@ -532,14 +542,17 @@ int lynx_hkv_dequant(const lynx_layout *L, int32_t b, int32_t T, const int32_t *
  *   parents      int32 [B][n] (device), as above
  *   out_bf16     BF16 [B][n][Hq][128] (device, written); rows of nodes that
  *                are not there are 0
- *   other arguments as lynx_attn_verify; workspace >=
- *   lynx_attn_workspace_bytes(L, B, Hq, n, max_seq_len)
+ *   other arguments as lynx_attn_verify
+ *   workspace    >= lynx_attn_workspace_bytes(L, B, Hq, n, max_seq_len).  Calls of
+ *                more than 64 rows a kv head (n Hq / num_kv_heads) over long
+ *                contexts take a kernel made for many rows where it holds
+ *                lynx_attn_tree_workspace_bytes(L, B, Hq, n, max_seq_len)
+ *                (2 x 64K tokens, 512 rows: 350 us instead of 566)
  * A node's K and V reach the rows of its descendants and its own alone,
  * whatever they hold (NaN and infinities included).
- * Precision: with up to 64 rows a kv head (n Hq / num_kv_heads), and with more
- * over short contexts, the context is attended as by lynx_attn_verify: there a
+ * Precision: but for that kernel the context is attended as by lynx_attn_verify: a
  * token's values lose bits where its V scale is 2^13 times smaller than the
- * largest of the context.  Otherwise a key is off by at most 2^-12 of the range
+ * largest of the context.  In that kernel a key is off by at most 2^-12 of the range
  * of its K group, a value by 2^-12 of itself (2^-40 of the largest), a weight by
  * 2^-12 of itself (2^-33 of the row's largest).  The choice goes by B, n and
  * max_seq_len, which is best near the lengths.

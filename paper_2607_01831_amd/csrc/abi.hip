@@ -182,10 +182,15 @@ size_t lynx_attn_workspace_bytes(const lynx_layout *L, int32_t B, int32_t Hq,
         max_seq_len < 0)
         return 0;
     const size_t bound = lynx::attention_workspace_bound(g, B, Hq, num_queries, max_seq_len);
-    // (a tree of as many nodes is one of the calls that it serves)
-    const size_t tree = lynx::tree_workspace_bound(g, B, Hq, num_queries, max_seq_len);
     const size_t limit = num_queries == 1 ? lynx::decode_limit_bytes(g, B, Hq, max_seq_len) : 0;
-    return std::max(std::max(bound, tree), limit);
+    return bound > limit ? bound : limit;
+}
+
+size_t lynx_attn_tree_workspace_bytes(const lynx_layout *L, int32_t B, int32_t Hq, int32_t n, int32_t max_seq_len) {
+    const size_t least = lynx_attn_workspace_bytes(L, B, Hq, n, max_seq_len);
+    Geometry g;
+    if (least == 0 || check_layout(L, &g) != LYNX_OK) return 0;
+    return std::max(least, lynx::tree_workspace_bound(g, B, Hq, n, max_seq_len));
 }
 
 int lynx_attn_anchor_decode(const lynx_layout *L, int32_t B, int32_t Hq, int32_t max_seq_len,
@@ -575,12 +580,13 @@ int lynx_internal_verify_tree(const lynx_layout *L, int32_t B, int32_t Hq, int32
     const void *ptrs[] = {k_new, v_new, parents};
     for (const void *p : ptrs)
         if (!p || !aligned16(p)) return LYNX_EINVAL;
-    const lynx::KvMode mode = wide < 0    ? lynx::tree_mode(g, B, Hq, n, max_seq_len)
+    const bool room = workspace_bytes >= lynx::tree_workspace_bound(g, B, Hq, n, max_seq_len);
+    const lynx::KvMode mode = wide < 0    ? (room ? lynx::tree_mode(g, B, Hq, n, max_seq_len) : lynx::KvMode::kCodes)
                               : wide == 0 ? lynx::KvMode::kCodes
                               : wide == 1 ? lynx::KvMode::kCodesWide
                                           : lynx::KvMode::kCodesHalfWide;
     const lynx::AttnPlan p = lynx::plan_attention(mode, g, B, Hq, n, max_seq_len);
-    const size_t bound = wide < 0 ? lynx::tree_workspace_bound(g, B, Hq, n, max_seq_len) : 0;
+    const size_t bound = wide < 0 ? lynx::attention_workspace_bound(g, B, Hq, n, max_seq_len) : 0;
     const size_t need = std::max(bound, p.workspace_bytes());
     if (!workspace || !aligned16(workspace) || workspace_bytes < need) return LYNX_EWORKSPACE;
     hipError_t e = lynx::launch_verify_tree(

@@ -213,7 +213,8 @@ hipError_t launch_anchor_split_decode(const SplitDecodeArgs &args, hipStream_t s
 AttnPlan plan_attention(KvMode mode, const Geometry &g, int B, int Hq, int nq, int max_seq_len,
                         size_t most = SIZE_MAX);
 // Workspace bytes that suffice for every decode and verification of at most B
-// sequences, nq queries each, and max_seq_len tokens; and for every tree.
+// sequences, nq queries each, and max_seq_len tokens, trees among them; and with
+// which a tree has every kernel to choose from.
 size_t attention_workspace_bound(const Geometry &g, int B, int Hq, int nq, int max_seq_len);
 size_t tree_workspace_bound(const Geometry &g, int B, int Hq, int n, int max_seq_len);
 // The kernel of a tree's context part: more rows a kv head than verify.hip's

@@ -91,6 +91,7 @@ def load():
         "lynx_kv_encode_split": ([LP, I32, I32, I32, P, P, P, P, P, P, P, MP, P], ctypes.c_int),
         "lynx_kv_merge_split": ([I32, SZ, P, P, P, P], ctypes.c_int),
         "lynx_kv_dequant_anchor_split": ([LP, I32, I32, I32, P, P, P, MP, P, P, P], ctypes.c_int),
+        "lynx_attn_tree_workspace_bytes": ([LP, I32, I32, I32, I32], SZ),
         "lynx_attn_verify_tree": ([P, I32, I32, I32, I32, P, P, P, P, P, P, P, P, P, P, P, SZ, P], ctypes.c_int),
         "lynx_spec_tree_workspace_bytes": ([I32, I32, I32], SZ),
         "lynx_spec_accept_tree_greedy": ([I32, I32, I32, P, P, P, P, P, P, P, SZ, P], ctypes.c_int),
@@ -331,11 +332,18 @@ def lynx_attn_workspace_bytes(L: Layout, B: int, Hq: int, num_queries: int,
 ATTN_COUNTER_BYTES = 262144
 
 
+def lynx_attn_tree_workspace_bytes(L: Layout, B: int, Hq: int, n: int, max_seq_len: int) -> int:
+    return int(load().lynx_attn_tree_workspace_bytes(ctypes.byref(L.c()), B, Hq, n, max_seq_len))
+
+
 def workspace(L: Layout, B: int, Hq: int, num_queries: int, max_seq_len: int,
-              device="cuda") -> torch.Tensor:
-    """A device buffer of lynx_attn_workspace_bytes() bytes (allocated by
-    torch), zero-filled: the arrival counters at its head must start at zero."""
-    n = lynx_attn_workspace_bytes(L, B, Hq, num_queries, max_seq_len)
+              device="cuda", tree: bool = True) -> torch.Tensor:
+    """A device buffer (allocated by torch) for any attention call of as many
+    queries, of lynx_attn_tree_workspace_bytes() bytes, or with tree=False of
+    lynx_attn_workspace_bytes(); zero-filled: the arrival counters at its head
+    must start at zero."""
+    size = lynx_attn_tree_workspace_bytes if tree else lynx_attn_workspace_bytes
+    n = size(L, B, Hq, num_queries, max_seq_len)
     return torch.zeros(max(n, ATTN_COUNTER_BYTES), dtype=torch.uint8, device=device)
 
 
