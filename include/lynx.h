@@ -679,7 +679,8 @@ int lynx_kv_append(const lynx_layout *L, int32_t B, int32_t max_new, int32_t n_s
  * quantize the open group from these values.
  *   seq_lens     int32 [B] (device): lengths; tokens past
  *                min(max_tokens, max_blocks_per_seq * bt) are ignored
- *   k_open       BF16 [B][LYNX_OPEN_ROWS][Hkv][128] (device, written)
+ *   k_open       BF16 [B][LYNX_OPEN_ROWS][Hkv][128] (device, written: the rows of
+ *                those tokens, 0 where the block id is outside [0, num_blocks))
  */
 int lynx_kv_append_begin(const lynx_layout *L, int32_t B, const int32_t *seq_lens,
                          const int32_t *block_table, const uint8_t *k_codes, const lynx_meta *meta,

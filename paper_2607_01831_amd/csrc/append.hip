@@ -260,12 +260,13 @@ __global__ __launch_bounds__(kThreads) void dequant_kernel(DequantArgs a) {
     const size_t vm = ((size_t)b * Hkv + h) * a.geo.max_tokens;
     uint2 c[PASSES];
     float2 sz[PASSES];
-    bool live[PASSES];
+    bool live[PASSES], held[PASSES];  // written; in the pool
 #pragma unroll
     for (int i = 0; i < PASSES; ++i) {
         const int at = t0 + tr + kStep * i, t = min(max(at, lo), hi - 1);  // rows outside the range repeat its nearest
         const long long row = pool_row(a.geo, bt_row, a.bt_shift, h, t);
-        live[i] = at == t && row >= 0;
+        held[i] = row >= 0;
+        live[i] = at == t && (RING || row >= 0);
         typedef unsigned int u32v2 __attribute__((ext_vector_type(2)));
         const u32v2 x = __builtin_nontemporal_load(
             reinterpret_cast<const u32v2 *>(codes + (row < 0 ? 0 : row) * kCodeRow + 8 * m));
@@ -297,6 +298,7 @@ __global__ __launch_bounds__(kThreads) void dequant_kernel(DequantArgs a) {
             const uint32_t w = (j < 4 ? c[i].x : c[i].y) >> (8 * (j & 3));
             o[j / 2] = pack_bf16(fmaf((float)(w & 0xFFu), sc[j], zr[j]), fmaf((float)((w >> 8) & 0xFFu), sc[j + 1], zr[j + 1]));
         }
+        if (RING && !held[i]) o = u32v4{0u, 0u, 0u, 0u};  // (the rows of a group decide its scale)
         const int t = t0 + tr + kStep * i;
         const size_t to = RING ? (size_t)(t % kRing) : (size_t)(t - first);
         u32v4 *p = reinterpret_cast<u32v4 *>(out + (to * Hkv + h) * kHeadDim + 8 * m);
