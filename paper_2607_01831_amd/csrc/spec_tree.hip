@@ -557,17 +557,18 @@ size_t spec_tree_workspace(int B, int n, int vocab) {
 }
 
 // Which kernel: the rows at once while reading them all takes no longer than
-// following a path of a few rows; at once and along the path, us.  Greedy, 4 kept:
-// 12.8M entries in all rows 13.2 and 15.5, 16.4M 16.2 and 16.0, 24.6M 20.4 and 18.2,
-// 65.7M 43.2 and 17.1.  Drawn, where a row on the path waits for its draw too, 4
-// kept: 12.8M 19.3 and 30.0, 24.6M 26.2 and 28.8, 25.6M 31.8 and 30.7, 32.8M 32.3 and
-// 29.5, 65.7M 65.6 and 29.1.  (A path as long as the tree is the other extreme: a
-// chain of 63, all kept, 16 sequences: 224 us along it, 97 at once.)  Chunks: 4096
-// entries where every row is read, 8192 along a path (16 sequences 20.2 us, by 4096
-// 25.2, by 16384 26.7).
+// following a path of a few rows; entries in all rows, at once and along the path, us.
+// Greedy, 4 kept: 13.3M 13.7 and 13.6, 16.2M 15.8 and 16.2, 16.4M 15.9 and 16.0 (16
+// sequences: 15.8 and 15.2), 16.7M 16.3 and 14.3, 24.6M 20.3 and 18.1, 65.7M 43.2 and
+// 17.1.  Drawn, where a row on the path waits for its draw too: 16.4M 20.3 and 28.6,
+// 22.3M 24.3 and 29.1, 24.6M 25.6 and 28.9 (16 sequences: 31.1 and 29.1), 26.7M 27.8
+// and 24.8, 65.7M 65.6 and 29.1.  What is kept is not known here, and a path as long
+// as the tree is the other extreme: a chain of 63, all kept, 16 sequences, 224 us
+// along it, 97 at once.  Chunks: 4096 entries where every row is read, 8192 along a
+// path (16 sequences 20.2 us, by 4096 25.2, by 16384 26.7).
 TreeAcceptWay spec_tree_way(int B, int n, int vocab, bool drawn) {
     const long long entries = (long long)B * (n + 1) * vocab;
-    return TreeAcceptWay{entries <= (drawn ? 27000000ll : 16777216ll), 128};
+    return TreeAcceptWay{entries <= (drawn ? 25000000ll : 16000000ll), 128};
 }
 
 hipError_t launch_spec_accept_tree(TreeAcceptArgs a, int B, TreeAcceptWay way, void *workspace, hipStream_t stream) {
