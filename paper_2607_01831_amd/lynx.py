@@ -194,14 +194,18 @@ def _attn_args(fn: str, L: "Layout", B: int, Hq: int, seq_lens, block_table, k_p
 
 
 def _here(stream):
-    """The current device and the stream of a call (without a CUDA context yet
-    there is no tensor to launch on)."""
+    """The current device and the stream of a call, one of that device (without a
+    CUDA context yet there is no tensor to launch on)."""
     if not torch.cuda.is_initialized():
         return 0, stream
     dev = torch._C._cuda_getDevice()
     if stream is None:
         return dev, torch._C._cuda_getCurrentRawStream(dev)
-    return dev, stream.cuda_stream if isinstance(stream, torch.cuda.Stream) else stream
+    if not isinstance(stream, torch.cuda.Stream):
+        return dev, stream
+    if stream.device_index != dev:
+        raise ValueError(f"the stream is one of device {stream.device_index}, not of the current one ({dev})")
+    return dev, stream.cuda_stream
 
 
 def _typed_form(fn: str, what: str, t, nbytes: int, dtype, dev: int):
