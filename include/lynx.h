@@ -547,7 +547,7 @@ size_t lynx_attn_tree_workspace_bytes(const lynx_layout *L, int32_t B, int32_t H
  *                more than 64 rows a kv head (n Hq / num_kv_heads) over long
  *                contexts take a kernel made for many rows where it holds
  *                lynx_attn_tree_workspace_bytes(L, B, Hq, n, max_seq_len)
- *                (2 x 64K tokens, 512 rows: 350 us instead of 566)
+ *                (2 x 64K tokens, 512 rows: 352 us instead of 552)
  * A node's K and V reach the rows of its descendants and its own alone,
  * whatever they hold (NaN and infinities included).
  * Precision: but for that kernel the context is attended as by lynx_attn_verify: a

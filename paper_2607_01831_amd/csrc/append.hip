@@ -11,7 +11,10 @@
 // What bounds it: a decode step's append moves at most 128 K rows of a head,
 // so it is a chain of dependent loads (length, rows, group extrema, stores); a
 // chunk of a prompt reads 4 bytes and writes 2 per element pair and is bound
-// by memory.
+// by memory: 4 x 4096 tokens of 8 heads 26.5 us into code planes (103 MB, 3.9 TB/s),
+// 27.4 into anchors and residuals, 24.8 into anchors alone, 31.8 into all; one token
+// of each of 16 sequences 7.1, and 7.7 into anchors and residuals; append_begin of
+// those 5.5.
 #include "lane_ops.h"
 #include "lynx_internal.h"
 #include "quantize.h"
@@ -229,10 +232,11 @@ __device__ __forceinline__ uint32_t pack_bf16(float a, float b) {
 // writes that have to be whole: a token's rows of all kv heads stand side by
 // side, so a workgroup takes HEADS heads of a few tokens and writes runs of 256
 // HEADS bytes (a workgroup per head of 128 tokens, runs of 256 bytes: 161 us for
-// 2 x 64K tokens of 8 heads).  Thread (row tid / 16 of 16: token, head; dims
+// 103K tokens of 8 heads in two sequences).  Thread (row tid / 16 of 16: token, head; dims
 // 8 m .. + 7) keeps its head's K scales and zeros, and loads its PASSES tokens'
-// codes before it uses any.  Codes and values go past the caches: 2 x 64K tokens
-// 124 us (5.2 TB/s, a copy's rate), with cached loads 147, cached stores too 155.
+// codes before it uses any.  Codes and values go past the caches: those tokens 124 us
+// (645 MB, 5.2 TB/s, a copy's rate), with cached loads 147, cached stores too 155;
+// 2 x 65536 tokens 159 us (822 MB, 5.2 TB/s).
 // RING: K alone, the open group and the one before it, into the ring; else
 // tokens starts[b] .. + counts[b] - 1, to row t - starts[b] of the output.
 template <bool RING, int HEADS, int PASSES>
@@ -308,7 +312,7 @@ __global__ __launch_bounds__(kThreads) void dequant_kernel(DequantArgs a) {
 
 template <bool RING, int HEADS>
 void launch_dequant_heads(DequantArgs a, int B, int rows, hipStream_t stream) {
-    constexpr int kPasses = 4;  // (8: 139 us for 2 x 64K tokens, 8.9 for 16 x 128; 4: 124 and 4.7)
+    constexpr int kPasses = 4;  // (8: 139 us for 103K tokens, 8.9 for 16 x 128; 4: 124 and 4.7)
     constexpr int kTokens = 16 / HEADS * kPasses;
     static_assert(kKGroup % kTokens == 0, "a workgroup stays in one K group");
     constexpr int kMostUnits = 65535;  // of a grid; more rows (524K at 8 heads) take a launch more

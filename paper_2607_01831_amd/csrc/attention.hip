@@ -513,12 +513,14 @@ size_t tree_workspace_bound(const Geometry &g, int B, int Hq, int n, int max_seq
 // The kernel of least estimated time.  verify.hip's serves 32 rows a workgroup, a
 // wide one kWideRows or half of them, whether they are there or not, and a
 // segment of it costs more to begin and to join; per token of a compute unit's
-// share and chunk of rows they take some 10.3, 43.7 and 27.2 ns.  Measured, us, 2
-// sequences of 64K (4096 tokens a unit) of 8 kv heads, narrow, wide and half: 80
-// rows 144, 198, 135; 128 rows 181, 202, 139; 160 rows 227, 204, 240; 256 rows 321,
-// 210, 244; of 16K (1024): 128 rows 53, 68, 55; 192 rows 74, 73, 78; 256 rows 84, 75,
-// 78; of 8K: 128 rows 36, 45, 40; 256 rows 51, 57, 54; 512 rows 84, 73, 78.  16 paged
-// sequences of 1K-8K: 100 rows 136, 168, 123; 256 rows 248, 189, 222.
+// share and chunk of rows they take some 10.3, 43.7 and 27.2 ns.  The tokens are
+// max_seq_len's: the lengths are on the device.  Measured, us, 2 sequences of 64K
+// (4096 tokens a unit) of 8 kv heads, narrow, wide and half: 80 rows 138, 197, 131;
+// 128 rows 169, 185, 128; 160 rows 209, 185, 225; 256 rows 310, 213, 246; 512 rows
+// 552, 352, 428; of 16K (1024): 128 rows 50, 66, 53; 192 rows 70, 70, 75; 256 rows
+// 80, 75, 78; of 8K: 128 rows 34, 44, 39; 256 rows 48, 55, 53; 512 rows 79, 72, 77.
+// 16 paged sequences of 1K-8K (71K tokens where 131K are taken): 100 rows 103, 140,
+// 106; 256 rows (81K) 210, 170, 201.
 KvMode tree_mode(const Geometry &g, int B, int Hq, int n, int max_seq_len) {
     const int rows = n * (Hq / g.Hkv);
     if (rows <= kNarrowRows) return KvMode::kCodes;  // (two chunks of 32 cost less than one of either)

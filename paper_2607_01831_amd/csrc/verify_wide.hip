@@ -36,18 +36,20 @@
 // with a wavefront's two partners each on one (TS 2; they join at the end).  A
 // tile costs a wavefront 34 MFMAs for its 32 rows (two of them sum the weights,
 // as a column of ones behind the values).  Iteration j: copies of step j + 4 into
-// LDS (asynchronous), the scores of step j + 1 in turns with the weights of step
-// j, the products with the values in turns with the conversion of step j + 2; one
-// barrier.  2 x 64K tokens, 8 kv heads, with the merge: 512 rows 341 us (verify.hip's
-// kernel 560), 128 rows 139 (181).  What bounds it: instructions.  A SIMD has two
-// wavefronts; behind an MFMA's 16 cycles two vector instructions are free and each
-// further one takes 5, and a wavefront's tile has 34 MFMAs and some 135 others,
-// 2000 of the 3200 cycles that it takes; the rest are the barrier and the waits
-// around it.  Without the conversion it would take 33 us less of 200 (256 rows),
-// without the copies 23, without the scores' products 30.  Tried: fragments and
-// codes read a step ahead of the barrier (347 and 170 us: registers), four
-// wavefronts of 32 rows twice on a CU (470), four of 64 rows (627), 128 rows by 16
-// a wavefront (152), two orders of the stretches for the wavefronts of a SIMD (444).
+// LDS (asynchronous), what step j + 3 needs of its metadata, the scores of step
+// j + 1 in turns with the weights of step j, the products with the values in turns
+// with the conversion of step j + 2; one barrier.  2 x 64K tokens, 8 kv heads, with
+// the merge: 512 rows 352 us (verify.hip's kernel 552), 128 rows 128 (169).  What
+// bounds it: no unit alone.  By its counters (512 rows) a wavefront's tile has 34
+// MFMAs, 124 other vector instructions and 29 of LDS, and of the 2950 cycles that it
+// takes the matrix cores are busy 37%, the vector units 47%, LDS 34%; behind an
+// MFMA's 16 cycles two vector instructions are free and each further one takes 5,
+// 1650 cycles for a SIMD's two wavefronts, and the rest are the barrier and the waits
+// around it.  Tried: fragments and codes read a step ahead of the barrier (347 and
+// 170 us where 341 and 139 were: registers), four wavefronts of 32 rows twice on a CU
+// (470), four of 64 rows (627), 128 rows by 16 a wavefront (152), two orders of the
+// stretches for the wavefronts of a SIMD (444), conversions by v_fma_mix (357 for
+// 350).
 #include "f16_ops.h"
 #include "lane_ops.h"
 #include "lynx_internal.h"
