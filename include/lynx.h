@@ -553,9 +553,9 @@ size_t lynx_attn_tree_workspace_bytes(const lynx_layout *L, int32_t B, int32_t H
  * Precision: but for that kernel the context is attended as by lynx_attn_verify: a
  * token's values lose bits where its V scale is 2^13 times smaller than the
  * largest of the context.  In that kernel a key is off by at most 2^-12 of the range
- * of its K group, a value by 2^-12 of itself (2^-40 of the largest), a weight by
- * 2^-12 of itself (2^-33 of the row's largest).  The choice goes by B, n and
- * max_seq_len, which is best near the lengths.
+ * of its K group (2^-39 of the channel's largest), a value by 2^-12 of itself
+ * (2^-40 of the largest), a weight by 2^-12 of itself (2^-33 of the row's
+ * largest).  The choice goes by B, n and max_seq_len, which is best near the lengths.
  */
 int lynx_attn_verify_tree(const lynx_layout *L, int32_t B, int32_t Hq, int32_t n,
                           int32_t max_seq_len, const int32_t *seq_lens, const int32_t *block_table,

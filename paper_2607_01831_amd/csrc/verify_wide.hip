@@ -11,12 +11,12 @@
 // order in LDS, and the queries are converted once.
 //
 // Operands:
-//  * K' = (zero + code scale - c) 2^(15 - e_d), e_d the exponent of the largest |K| of
+//  * K' = (zero + code scale - c) 2^(14 - e_d), e_d the exponent of the largest |K| of
 //    channel d in the segment (from the metadata), c a number inside the range of the
 //    group: 0 at first, and from group to group moved to the range's end where it is
-//    outside.  K' is computed in fp32 and rounded to fp16 once: a key is off by 2^-12
+//    outside, so |K'| <= 2^15.  K' is computed in fp32 and rounded to fp16 once: a key is off by 2^-12
 //    of its group's range at most, a sixteenth of a code's step (of itself where c is
-//    0; and by 2^-40 of the channel's largest where it is a subnormal).  So neither
+//    0; and by 2^-39 of the channel's largest where it is a subnormal).  So neither
 //    what the keys of a group have in common, which the softmax does not see, nor a
 //    token far from the others takes bits from the rest.  sum_d q_d c_d, of exact
 //    products (c has fp16's 11 bits), is added to the scores in fp32, where they
@@ -73,6 +73,7 @@ constexpr int kFragBytes = 8 * 1024;                // a tile's 8 fragments of K
 constexpr int kFragsV = 3;                          // V's buffers; K's are two
 constexpr int kDepth = 4;                           // steps whose copies are in flight or not converted yet
 constexpr int kUpper = 15;                          // fp16 operands reach up to 2^15
+constexpr int kUpperK = kUpper - 1;                 // keys before c is taken off, which may be at the other end
 constexpr float kSlack = 7.0f;                      // log2 units that the reference may lag behind
 constexpr float kLift = kUpper - kSlack;            // ... that weights are held above it
 
@@ -296,7 +297,7 @@ __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<
             }
         // positive and finite: times the -inf of a token past the context it must
         // not be a NaN
-        sc[rt] = __builtin_amdgcn_fmed3f(ldexpf(kLog2e * rsqrtf((float)kHeadDim), E - 2 * kUpper), FLT_MIN, FLT_MAX);
+        sc[rt] = __builtin_amdgcn_fmed3f(ldexpf(kLog2e * rsqrtf((float)kHeadDim), E - kUpper - kUpperK), FLT_MIN, FLT_MAX);
     }
 
     // ---- conversion of a step into operand order ----
@@ -307,7 +308,7 @@ __device__ __forceinline__ void wide_segment(const VerifyArgs &a, const Segment<
     auto prepare = [&](int g) {  // a thread per channel
         if (w >= kHeadDim / 64) return;
         const float *km = s_km[g % 3];
-        const int up = kUpper - s_e[tid];
+        const int up = kUpperK - s_e[tid];
         const float scale = ldexpf(km[tid], up), zero = ldexpf(km[kHeadDim + tid], up);
         const float was = g > 0 ? (float)s_c[~g & 1][tid] : 0.0f;
         const _Float16 c = (_Float16)__builtin_amdgcn_fmed3f(was, zero, fmaf(255.0f, scale, zero));

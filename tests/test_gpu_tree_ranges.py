@@ -194,3 +194,16 @@ def small_groups(k, v, q):
 def test_groups_of_other_sizes(wide):
     c, *x = made([1500, 333], 2, small_groups)
     check(c, *x, wide, random_parents(2, 30, seed=4))
+
+
+@pytest.mark.parametrize("wide", [0, 1, 2])
+@pytest.mark.parametrize("sign", [1, -1])
+def test_a_group_at_one_end_then_one_over_the_whole_range(sign, wide):
+    """Keys less the number that the group before left: twice the largest key, of scales
+    and zeros that are no BF16."""
+    c, q, kn, vn = made([1500, 333], 2, lambda k, v, q: None)
+    m, end = c.pool.meta, 8.0 * (1 - 2.0 ** -14)
+    for d in (5, 77):
+        m.k_scale[:, :, 0::2, d], m.k_zero[:, :, 0::2, d] = 2.0 ** -20, sign * (end - 2.0 ** -11)
+        m.k_scale[:, :, 1::2, d], m.k_zero[:, :, 1::2, d] = 2 * end / 255, -end
+    check(c, q, kn, vn, wide, random_parents(2, 30, seed=4))
