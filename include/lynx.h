@@ -705,6 +705,141 @@ int lynx_kv_dequant(const lynx_layout *L, int32_t B, int32_t max_n, const int32_
                     const uint8_t *v_codes, const lynx_meta *meta, void *k_out_bf16,
                     void *v_out_bf16, void *stream);
 
+/*
+ * lynx_attn_hier -- attention over the hierarchical codec's cache (Alg. 1; the
+ * attention of Sec. 2), read straight from its planes: for every sequence and
+ * query, O = softmax(q K^T / sqrt(128)) V over the context, with
+ * x = ((+-level(code) * sigma) + mu) * gscale + gmin as lynx_hkv_dequant defines
+ * it but not rounded to BF16, and over the BF16 tokens behind it.  One query a
+ * sequence is decoding, with the tokens generated since as the tail; k queries
+ * and as many tail tokens are the verification of k drafts (Sec. 4.3).
+ *
+ *   k            queries per sequence, 1 <= k <= 64; B <= 65535
+ *   full         0: k_plane and v_plane are 4-bit planes (anchors, or the single
+ *                4-bit code of LYNX_HQ_INT4); 1: the merged codes of
+ *                lynx_kv_merge (not for LYNX_HQ_INT4: LYNX_EINVAL)
+ *   alpha, variant  those of lynx_hkv_encode
+ *   q_bf16       BF16 [B][k][Hq][128] (device)
+ *   n_tail       tokens behind the context, 0 or k <= n_tail <= 64; query i sees
+ *                the first n_tail - k + i + 1 of them
+ *   k_tail, v_tail  BF16 [B][n_tail][Hkv][128] (device); not read if n_tail == 0
+ *   out_bf16     BF16 [B][k][Hq][128] (device, written)
+ *   lse          fp32 [B][k][Hq] as for lynx_attn_anchor_decode, or NULL
+ *   other arguments as lynx_attn_anchor_decode; workspace >=
+ *   lynx_attn_workspace_bytes(L, B, Hq, k, max_seq_len), its arrival counters
+ *   zero on entry (every call leaves them zero)
+ * A query that sees no token yields zeros and lse = -inf; the rows of a sequence
+ * one of whose block ids is outside [0, num_blocks) are NaN.
+ * Precision: with b = sigma * gscale and m = mu * gscale + gmin, a key or value
+ * x = +-level b + m of the context is off by at most 2^-11 (2 |level b| + |m| + |x|)
+ * (2^-37 of the largest of the context), a weight by 2^-11 of itself (2^-32 of the
+ * row's largest).
+ */
+int lynx_attn_hier(const lynx_layout *L, int32_t B, int32_t Hq, int32_t k, int32_t max_seq_len,
+                   const int32_t *seq_lens, const int32_t *block_table, int32_t full,
+                   const uint8_t *k_plane, const uint8_t *v_plane, float alpha, int32_t variant,
+                   const lynx_hmeta *meta, const void *q_bf16, int32_t n_tail, const void *k_tail,
+                   const void *v_tail, void *out_bf16, float *lse, void *workspace,
+                   size_t workspace_bytes, void *stream);
+
+/*
+ * lynx_qk_norm_rope -- what stands between a layer's projections and the calls
+ * above: the norm of every query and key head and the rotation by its token's
+ * position, in one pass, written to the rows that q, k_new, v_new and the tails
+ * of those calls are.  Per head of 128 dims, in fp32, rounded to BF16 once:
+ *   y = x * rsqrt(mean(x^2) + eps) * weight, or x where the weights are NULL;
+ *   of the first rotary_dim dims, pairs (a, b) become
+ *   (a cos - b sin, b cos + a sin) * scale with the angle position * inv_freq[i],
+ *   taken exactly however far the position is.
+ * V is moved as it is.
+ *
+ *   head_dim     must be 128 (LYNX_ENOTSUP)
+ *   q, k, v      BF16 heads: token n's at element n * stride (a stride of at
+ *                least heads * 128, a multiple of 8: the three may be parts of
+ *                one fused row); v and v_out may be NULL, both
+ *   positions    int32 [n_tokens] (device); a token of negative position is not
+ *                there: nothing is written for it
+ *   rows         int32 [n_tokens] (device): the output row of each token; tokens
+ *                whose row is outside [0, n_rows) are skipped.  Or NULL: row n,
+ *                and n_rows >= n_tokens.  A row stands once at most
+ *   n_rows       rows of the outputs
+ *   q_weight, k_weight  BF16 [128] (device), or NULL: no norm
+ *   inv_freq     fp32 [rotary_dim / 2] (device); NULL if rotary_dim == 0
+ *   rotary_dim   0..128, a multiple of 16
+ *   pairs        0: dims i and i + rotary_dim / 2 are a pair; 1: 2 i and 2 i + 1
+ *   scale        of the rotated dims (1, or a long-context factor)
+ *   q_out        BF16 [n_rows][Hq][128]; k_out, v_out BF16 [n_rows][Hkv][128]
+ *                (device, written; rows of no token are left as they were; none
+ *                may overlap an input)
+ */
+int lynx_qk_norm_rope(int32_t n_tokens, int32_t Hq, int32_t Hkv, int32_t head_dim,
+                      const void *q_bf16, int64_t q_stride, const void *k_bf16, int64_t k_stride,
+                      const void *v_bf16, int64_t v_stride, const int32_t *positions,
+                      const int32_t *rows, int32_t n_rows, const void *q_weight,
+                      const void *k_weight, float eps, const float *inv_freq, int32_t rotary_dim,
+                      int32_t pairs, float scale, void *q_out, void *k_out, void *v_out,
+                      void *stream);
+
+/*
+ * The blocks of a paged cache, kept on the device.  A stack holds the blocks that
+ * no sequence has:
+ *   free_blocks  int32 [num_blocks]: its ids, entry 0 at the bottom
+ *   free_state   int32 [2] (16-byte aligned): the number of ids on it, and a word
+ *                that is 0 before the first call and that every call leaves 0
+ * Calls that share a stack must not run concurrently.
+ */
+
+/*
+ * lynx_blocks_extend -- the plan of a step: room for new tokens behind every
+ * sequence, and where each of them goes.  A sequence of length n holds the first
+ * ceil(n / block_tokens) entries of its block_table row; the blocks that its new
+ * tokens need beyond those come off the stack, the first sequence's first block
+ * from the top.  A sequence is granted all of its tokens or none: it is refused if
+ * it needs a block and the blocks that it and the sequences before it need are
+ * more than the stack holds, or if the tokens that it and the sequences before it
+ * ask for are more than max_rows (refused sequences count in both).
+ *
+ *   n_src        tokens per sequence at most; B * n_src < 2^31
+ *   max_rows     entries of the token arrays (<= 2^30)
+ *   seq_lens     int32 [B] (device): lengths before the step (not changed),
+ *                clamped to 0 .. C = min(max_tokens, max_blocks_per_seq * bt)
+ *   counts       int32 [B] (device): tokens asked for, clamped to 0..n_src and to
+ *                what C leaves room for
+ *   block_table  int32 [B][max_blocks_per_seq] (device): the new blocks' entries
+ *                are written, no other
+ *   granted      int32 [B] (device, written): counts, or 0 where refused
+ *   starts       int32 [B+1] (device, written): granted tokens of the sequences
+ *                before; starts[B] of all
+ *   seq_of, positions, slots, rows   int32 [max_rows] (device, written), each may
+ *                be NULL: of token n (sequence-major) its sequence b; its position
+ *                p; block_table[b][p / bt] * bt + p % bt, -1 where that block id is
+ *                outside [0, num_blocks); and its row b * n_src + i in arrays
+ *                [B][n_src] (new token i of the sequence), as `rows` of
+ *                lynx_qk_norm_rope fills them.  -1 from starts[B] on
+ * granted and starts must not be counts or seq_lens; num_blocks * block_tokens and
+ * B * max_blocks_per_seq must be less than 2^31.  B <= 65535.  Launches one kernel.
+ */
+int lynx_blocks_extend(const lynx_layout *L, int32_t B, int32_t n_src, int32_t max_rows,
+                       const int32_t *seq_lens, const int32_t *counts, int32_t *block_table,
+                       const int32_t *free_blocks, int32_t *free_state, int32_t *granted,
+                       int32_t *starts, int32_t *seq_of, int32_t *positions, int32_t *slots,
+                       int32_t *rows, void *stream);
+
+/*
+ * lynx_blocks_release -- blocks go back to the stack: those of every sequence that
+ * no token before keep[b] is in (drafts dropped; keep 0: the sequence is done).
+ *   seq_lens     int32 [B] (device): lengths so far, clamped as above
+ *   keep         int32 [B] (device): lengths from now on, clamped to 0..seq_lens[b]
+ *   block_table  the entries of those blocks become -1
+ *   free_blocks, free_state   the ids are pushed so that the first sequence's first
+ *                block is on top: releasing what an extend took restores the stack.
+ *                Ids that num_blocks leaves no room for are dropped
+ * Launches one kernel.
+ */
+int lynx_blocks_release(const lynx_layout *L, int32_t B, const int32_t *seq_lens,
+                        const int32_t *keep, int32_t *block_table, int32_t *free_blocks,
+                        int32_t *free_state, void *stream);
+
 /* Static, human-readable text for a lynx_status value. */
 const char *lynx_strerror(int status);
 

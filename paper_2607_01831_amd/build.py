@@ -16,8 +16,9 @@ CSRC = HERE / "csrc"
 ROOT = HERE.parent
 LIBRARY = HERE / "liblynx.so"
 ARGS = HERE / "_args.so"
-SOURCES = ["codec.hip", "hier.hip", "attention.hip", "anchor_decode.hip", "anchor_split.hip", "verify.hip",
-           "verify_wide.hip", "tree.hip", "append.hip", "spec.hip", "spec_tree.hip", "abi.hip"]
+SOURCES = ["codec.hip", "hier.hip", "hier_attn.hip", "attention.hip", "anchor_decode.hip", "anchor_split.hip", "verify.hip",
+           "verify_wide.hip", "tree.hip", "append.hip", "spec.hip", "spec_tree.hip", "rope.hip", "blocks.hip",
+           "abi.hip"]
 HIPCC = os.environ.get("HIPCC", "/opt/rocm/bin/hipcc")
 
 FLAGS = [

@@ -4,6 +4,8 @@
 #include "../../include/lynx.h"
 #include "lynx_internal.h"
 
+#include <math.h>
+
 #include <algorithm>
 #include <mutex>
 
@@ -759,6 +761,163 @@ int lynx_kv_dequant(const lynx_layout *L, int32_t B, int32_t max_n, const int32_
     a.k_out = static_cast<uint16_t *>(k_out_bf16);
     a.v_out = static_cast<uint16_t *>(v_out_bf16);
     hipError_t e = lynx::launch_dequant(a, B, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? LYNX_OK : LYNX_EHIP;
+}
+
+int lynx_attn_hier(const lynx_layout *L, int32_t B, int32_t Hq, int32_t k, int32_t max_seq_len,
+                   const int32_t *seq_lens, const int32_t *block_table, int32_t full, const uint8_t *k_plane,
+                   const uint8_t *v_plane, float alpha, int32_t variant, const lynx_hmeta *meta, const void *q_bf16,
+                   int32_t n_tail, const void *k_tail, const void *v_tail, void *out_bf16, float *lse,
+                   void *workspace, size_t workspace_bytes, void *stream) {
+    Geometry g;
+    lynx::HMetaPtrs hp;
+    int rc = check_layout(L, &g);
+    if (rc != LYNX_OK) return rc;
+    if ((rc = check_hmeta(meta, &hp)) != LYNX_OK) return rc;
+    if (!alpha_ok(alpha) || !variant_ok(variant) || (full != 0 && full != 1) ||
+        (full == 1 && variant == LYNX_HQ_INT4))
+        return LYNX_EINVAL;
+    if (B < 0 || B > kMostB || Hq < 1 || Hq % g.Hkv != 0 || k < 1 || k > 64 || max_seq_len < 0 ||
+        max_seq_len > layout_capacity(g))
+        return LYNX_EINVAL;
+    if (n_tail != 0 && (n_tail < k || n_tail > 64)) return LYNX_EINVAL;
+    if (B == 0) return LYNX_OK;
+    const void *ptrs[] = {seq_lens, block_table, k_plane, v_plane, q_bf16, out_bf16};
+    for (const void *p : ptrs)
+        if (!p || !aligned16(p)) return LYNX_EINVAL;
+    if (n_tail > 0 && (!k_tail || !v_tail || !aligned16(k_tail) || !aligned16(v_tail))) return LYNX_EINVAL;
+    if (!aligned16(lse)) return LYNX_EINVAL;
+    const lynx::AttnPlan p = lynx::plan_attention(lynx::KvMode::kHier, g, B, Hq, k, max_seq_len);
+    if (!workspace || !aligned16(workspace) ||
+        workspace_bytes < lynx::attention_workspace_bound(g, B, Hq, k, max_seq_len))
+        return LYNX_EWORKSPACE;
+    hipError_t e = lynx::launch_attn_hier(
+        g, p, B, Hq, k, max_seq_len, seq_lens, block_table, full == 1, k_plane, v_plane, alpha, variant, hp,
+        static_cast<const uint16_t *>(q_bf16), n_tail, static_cast<const uint16_t *>(k_tail),
+        static_cast<const uint16_t *>(v_tail), static_cast<uint16_t *>(out_bf16), lse, workspace,
+        static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? LYNX_OK : LYNX_EHIP;
+}
+
+int lynx_qk_norm_rope(int32_t n_tokens, int32_t Hq, int32_t Hkv, int32_t head_dim, const void *q_bf16,
+                      int64_t q_stride, const void *k_bf16, int64_t k_stride, const void *v_bf16, int64_t v_stride,
+                      const int32_t *positions, const int32_t *rows, int32_t n_rows, const void *q_weight,
+                      const void *k_weight, float eps, const float *inv_freq, int32_t rotary_dim, int32_t pairs,
+                      float scale, void *q_out, void *k_out, void *v_out, void *stream) {
+    if (head_dim != lynx::kHeadDim) return LYNX_ENOTSUP;
+    if (n_tokens < 0 || n_rows < 0 || Hq < 1 || Hkv < 1 || Hq > (1 << 16) || Hkv > (1 << 16)) return LYNX_EINVAL;
+    if (rotary_dim < 0 || rotary_dim > lynx::kHeadDim || rotary_dim % 16 != 0 || (pairs != 0 && pairs != 1))
+        return LYNX_EINVAL;
+    if (!(eps >= 0.0f) || isinf(eps) || !isfinite(scale)) return LYNX_EINVAL;
+    if (!rows && n_rows < n_tokens) return LYNX_EINVAL;
+    if ((v_bf16 == nullptr) != (v_out == nullptr)) return LYNX_EINVAL;
+    if (n_tokens == 0) return LYNX_OK;
+    const int64_t strides[] = {q_stride, k_stride, v_bf16 ? v_stride : (int64_t)Hkv * lynx::kHeadDim};
+    for (int i = 0; i < 3; ++i)
+        if (strides[i] < (int64_t)(i == 0 ? Hq : Hkv) * lynx::kHeadDim || strides[i] % 8 != 0 ||
+            strides[i] > ((int64_t)1 << 31))
+            return LYNX_EINVAL;
+    const void *ptrs[] = {q_bf16, k_bf16, positions, q_out, k_out};
+    for (const void *p : ptrs)
+        if (!p || !aligned16(p)) return LYNX_EINVAL;
+    const void *may_be_null[] = {v_bf16, v_out, rows, q_weight, k_weight, inv_freq};
+    for (const void *p : may_be_null)
+        if (!aligned16(p)) return LYNX_EINVAL;
+    if (rotary_dim > 0 && !inv_freq) return LYNX_EINVAL;
+    lynx::RopeArgs a;
+    a.n_tokens = n_tokens;
+    a.Hq = Hq;
+    a.Hkv = Hkv;
+    a.rotary = rotary_dim;
+    a.pairs = pairs;
+    a.n_rows = n_rows;
+    a.q_stride = q_stride;
+    a.k_stride = k_stride;
+    a.v_stride = v_stride;
+    a.q = static_cast<const uint16_t *>(q_bf16);
+    a.k = static_cast<const uint16_t *>(k_bf16);
+    a.v = static_cast<const uint16_t *>(v_bf16);
+    a.positions = positions;
+    a.rows = rows;
+    a.q_weight = static_cast<const uint16_t *>(q_weight);
+    a.k_weight = static_cast<const uint16_t *>(k_weight);
+    a.eps = eps;
+    a.scale = scale;
+    a.inv_freq = inv_freq;
+    a.q_out = static_cast<uint16_t *>(q_out);
+    a.k_out = static_cast<uint16_t *>(k_out);
+    a.v_out = static_cast<uint16_t *>(v_out);
+    hipError_t e = lynx::launch_rope(a, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? LYNX_OK : LYNX_EHIP;
+}
+
+}  // extern "C"
+
+namespace {
+// What the two block calls share.
+int blocks_args(const lynx_layout *L, int32_t B, const int32_t *seq_lens, const int32_t *counts, int32_t *block_table,
+                int32_t *free_blocks, int32_t *free_state, lynx::BlocksArgs *a) {
+    Geometry g;
+    int rc = check_layout(L, &g);
+    if (rc != LYNX_OK) return rc;
+    if (B < 0 || B > kMostB || (long long)B * g.max_blocks > INT32_MAX || (long long)g.num_blocks * g.bt > INT32_MAX)
+        return LYNX_EINVAL;
+    const void *ptrs[] = {seq_lens, counts, block_table, free_blocks, free_state};
+    for (const void *p : ptrs)
+        if (B > 0 && (!p || !aligned16(p))) return LYNX_EINVAL;
+    *a = lynx::BlocksArgs{};
+    a->B = B;
+    a->bt = g.bt;
+    a->max_blocks = g.max_blocks;
+    a->num_blocks = g.num_blocks;
+    a->capacity = (int)layout_capacity(g);
+    a->seq_lens = seq_lens;
+    a->counts = counts;
+    a->block_table = block_table;
+    a->free_blocks = free_blocks;
+    a->state = free_state;
+    return LYNX_OK;
+}
+}  // namespace
+
+extern "C" {
+
+int lynx_blocks_extend(const lynx_layout *L, int32_t B, int32_t n_src, int32_t max_rows, const int32_t *seq_lens,
+                       const int32_t *counts, int32_t *block_table, const int32_t *free_blocks, int32_t *free_state,
+                       int32_t *granted, int32_t *starts, int32_t *seq_of, int32_t *positions, int32_t *slots,
+                       int32_t *rows, void *stream) {
+    lynx::BlocksArgs a;
+    int rc = blocks_args(L, B, seq_lens, counts, block_table, const_cast<int32_t *>(free_blocks), free_state, &a);
+    if (rc != LYNX_OK) return rc;
+    if (n_src < 0 || (long long)B * n_src > INT32_MAX || max_rows < 0 || max_rows > (1 << 30)) return LYNX_EINVAL;
+    if (B == 0) return LYNX_OK;
+    const void *ptrs[] = {granted, starts};
+    for (const void *p : ptrs)
+        if (!p || !aligned16(p)) return LYNX_EINVAL;
+    const void *may_be_null[] = {seq_of, positions, slots, rows};
+    for (const void *p : may_be_null)
+        if (!aligned16(p)) return LYNX_EINVAL;
+    // what every workgroup reads is written by none
+    if (granted == counts || granted == seq_lens || starts == counts || starts == seq_lens) return LYNX_EINVAL;
+    a.n_src = n_src;
+    a.max_rows = max_rows;
+    a.granted = granted;
+    a.starts = starts;
+    a.seq_of = seq_of;
+    a.positions = positions;
+    a.slots = slots;
+    a.rows = rows;
+    hipError_t e = lynx::launch_blocks_extend(a, static_cast<hipStream_t>(stream));
+    return e == hipSuccess ? LYNX_OK : LYNX_EHIP;
+}
+
+int lynx_blocks_release(const lynx_layout *L, int32_t B, const int32_t *seq_lens, const int32_t *keep,
+                        int32_t *block_table, int32_t *free_blocks, int32_t *free_state, void *stream) {
+    lynx::BlocksArgs a;
+    int rc = blocks_args(L, B, seq_lens, keep, block_table, free_blocks, free_state, &a);
+    if (rc != LYNX_OK) return rc;
+    if (B == 0) return LYNX_OK;
+    hipError_t e = lynx::launch_blocks_release(a, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? LYNX_OK : LYNX_EHIP;
 }
 

@@ -26,7 +26,7 @@ struct AttnArgs {
     int B, Hq, nq, G, max_seq_len;
     int rows_total, direct, workers, n_seg, max_live;
     int tail;             // attend the BF16 tail
-    int tail_count;       // tokens of the tail every query sees; -1: query i sees i + 1 (drafts)
+    int tail_first;       // tokens of the tail that query 0 sees; query i sees i more
     int tail_stride;      // tail tokens stored per sequence in k_new / v_new
     const int32_t *seq_lens;
     const uint16_t *q;
@@ -77,11 +77,11 @@ __global__ __launch_bounds__(kCombineThreads) void attn_combine_kernel(AttnArgs 
 
     // query row gr <-> (query qi, head qg); with a tail, query qi also sees
     // the BF16 tokens of the tail: drafts 0..qi in verification (causal among
-    // the drafts), all tail_count generated tokens in decode
+    // the drafts), all generated tokens in decode
     const int qi = gr / a.G;
     const int qg = gr % a.G;
     const size_t qrow = ((size_t)b * a.nq + qi) * a.Hq + (size_t)h * a.G + qg;
-    const int n_tail = a.tail ? (a.tail_count < 0 ? qi + 1 : a.tail_count) : 0;
+    const int n_tail = a.tail ? a.tail_first + qi : 0;
 
     const int d4 = tid % (kHeadDim / 4);
     const int sg = tid / (kHeadDim / 4);
@@ -264,9 +264,8 @@ __global__ __launch_bounds__(32 * ROWS) void attn_combine_rows_kernel(AttnArgs a
     const int qi = gr / a.G;
     const size_t qrow = ((size_t)b * a.nq + qi) * a.Hq + (size_t)h * a.G + gr % a.G;
     // tail tokens of this row, and of any row of the workgroup
-    const int n_tail = a.tail ? (a.tail_count < 0 ? qi + 1 : a.tail_count) : 0;
-    const int tail_most =
-        a.tail ? (a.tail_count < 0 ? (min(row0 + ROWS, a.rows_total) - 1) / a.G + 1 : a.tail_count) : 0;
+    const int n_tail = a.tail ? a.tail_first + qi : 0;
+    const int tail_most = a.tail ? a.tail_first + (min(row0 + ROWS, a.rows_total) - 1) / a.G : 0;
     __shared__ __attribute__((aligned(16))) uint4 s_v[kTailMax * (kHeadDim / 8)];  // tail values
     // queries, a thread's 32 dims 4 floats past the last's: other banks
     __shared__ __attribute__((aligned(16))) float s_q[ROWS][kHeadDim + 16];
@@ -448,7 +447,8 @@ AttnPlan plan_attention(KvMode mode, const Geometry &g, int B, int Hq, int nq, i
     p.rows_total = nq * (Hq / g.Hkv);
     // rows per workgroup
     const bool wide = mode == KvMode::kCodesWide || mode == KvMode::kCodesHalfWide;
-    const int tile = wide ? wide_rows(mode) : mode == KvMode::kCodes && p.rows_total > 16 ? 32 : 16;
+    const bool two = (mode == KvMode::kCodes || mode == KvMode::kHier) && p.rows_total > 16;
+    const int tile = wide ? wide_rows(mode) : two ? 32 : 16;
     const long long chunks = (p.rows_total + tile - 1) / tile;
     // (a wide workgroup is the only one of its CU)
     const long long slots = wide ? resident_workgroups() / 2 : resident_workgroups();
@@ -637,6 +637,36 @@ hipError_t launch_verify_tree(KvMode mode, const Geometry &g, const AttnPlan &pl
     return launch_tree_combine(a, each > 4 && fours <= resident_workgroups() ? 4 : 16, stream);
 }
 
+// The merge of the partials of `plan` and the tail.
+static hipError_t launch_combine(const AttnArgs &a, const AttnPlan &plan, uint16_t *out, float *lse, hipStream_t stream) {
+    // Many partials a sequence: a row per workgroup, 8 threads deep in them, while
+    // those workgroups are resident at once; else the rows share workgroups.
+    // Many are more than the 8 that a thread loads together where the partials
+    // are found without the list (2 sequences of 8K, 2 drafts, 128 rows of 16
+    // partials: 16.8 us, shared 18.2; 2048 such rows: 33.9, shared 26.4), and
+    // more than 16 with it (8 of 1.5K-5K, 2 drafts, 9 partials: 20.6, shared
+    // 19.9; 2 of 19K, 33 partials: 26.1, shared 29.8).  A single sequence's rows
+    // of more than 16 go alone whatever their number (32K, 20 drafts, 640 rows:
+    // 46.2, shared 47.7).
+    const int each = plan.direct ? plan.direct : std::min(plan.max_live, plan.workers / a.B + 1);
+    const long long rows_all = (long long)plan.rows_total * a.geo.Hkv * a.B;
+    const bool deep = (each > (plan.direct ? 8 : 16) && rows_all <= resident_workgroups()) || (a.B == 1 && each > 16);
+    if (!deep) {
+        const int find = plan.direct ? 0 : a.B > 1 && a.B <= 64 ? 1 : 2;
+        if (plan.rows_total <= 4)
+            launch_combine_rows<4>(find, a, out, lse, stream);
+        else
+            launch_combine_rows<8>(find, a, out, lse, stream);
+    } else if (plan.max_live <= 64) {
+        hipLaunchKernelGGL(attn_combine_kernel<8>, dim3(plan.rows_total, a.geo.Hkv, a.B), dim3(kCombineThreads),
+                           0, stream, a, out, lse);
+    } else {
+        hipLaunchKernelGGL(attn_combine_kernel<16>, dim3(plan.rows_total, a.geo.Hkv, a.B), dim3(kCombineThreads),
+                           0, stream, a, out, lse);
+    }
+    return hipGetLastError();
+}
+
 hipError_t launch_attention(KvMode mode, const Geometry &g, const AttnPlan &plan, int B, int Hq,
                             int nq, int max_seq_len, const int32_t *seq_lens,
                             const int32_t *block_table, const uint8_t *k_plane,
@@ -658,7 +688,7 @@ hipError_t launch_attention(KvMode mode, const Geometry &g, const AttnPlan &plan
     a.n_seg = plan.n_seg;
     a.max_live = plan.max_live;
     a.tail = k_new != nullptr ? 1 : 0;
-    a.tail_count = mode == KvMode::kCodes ? -1 : tail_count;
+    a.tail_first = mode == KvMode::kCodes ? 1 : tail_count;
     a.tail_stride = mode == KvMode::kCodes ? nq : tail_count;
     a.seq_lens = seq_lens;
     a.q = q;
@@ -750,32 +780,71 @@ hipError_t launch_attention(KvMode mode, const Geometry &g, const AttnPlan &plan
     } else {
         return hipErrorInvalidValue;  // anchor attention with several queries: no entry point asks for it
     }
-    // Many partials a sequence: a row per workgroup, 8 threads deep in them, while
-    // those workgroups are resident at once; else the rows share workgroups.
-    // Many are more than the 8 that a thread loads together where the partials
-    // are found without the list (2 sequences of 8K, 2 drafts, 128 rows of 16
-    // partials: 16.8 us, shared 18.2; 2048 such rows: 33.9, shared 26.4), and
-    // more than 16 with it (8 of 1.5K-5K, 2 drafts, 9 partials: 20.6, shared
-    // 19.9; 2 of 19K, 33 partials: 26.1, shared 29.8).  A single sequence's rows
-    // of more than 16 go alone whatever their number (32K, 20 drafts, 640 rows:
-    // 46.2, shared 47.7).
-    const int each = plan.direct ? plan.direct : std::min(plan.max_live, plan.workers / B + 1);
-    const long long rows_all = (long long)plan.rows_total * g.Hkv * B;
-    const bool deep = (each > (plan.direct ? 8 : 16) && rows_all <= resident_workgroups()) || (B == 1 && each > 16);
-    if (!deep) {
-        const int find = plan.direct ? 0 : B > 1 && B <= 64 ? 1 : 2;
-        if (plan.rows_total <= 4)
-            launch_combine_rows<4>(find, a, out, lse, stream);
-        else
-            launch_combine_rows<8>(find, a, out, lse, stream);
-    } else if (plan.max_live <= 64) {
-        hipLaunchKernelGGL(attn_combine_kernel<8>, dim3(plan.rows_total, g.Hkv, B), dim3(kCombineThreads),
-                           0, stream, a, out, lse);
-    } else {
-        hipLaunchKernelGGL(attn_combine_kernel<16>, dim3(plan.rows_total, g.Hkv, B), dim3(kCombineThreads),
-                           0, stream, a, out, lse);
-    }
-    return hipGetLastError();
+    return launch_combine(a, plan, out, lse, stream);
+}
+
+hipError_t launch_attn_hier(const Geometry &g, const AttnPlan &plan, int B, int Hq, int nq, int max_seq_len,
+                            const int32_t *seq_lens, const int32_t *block_table, bool full, const uint8_t *k_plane,
+                            const uint8_t *v_plane, float alpha, int variant, HMetaPtrs meta, const uint16_t *q,
+                            int n_tail, const uint16_t *k_tail, const uint16_t *v_tail, uint16_t *out, float *lse,
+                            void *workspace, hipStream_t stream) {
+    AttnArgs a;
+    a.geo = g;
+    a.B = B;
+    a.Hq = Hq;
+    a.nq = nq;
+    a.G = Hq / g.Hkv;
+    a.max_seq_len = max_seq_len;
+    a.rows_total = plan.rows_total;
+    a.direct = plan.direct;
+    a.workers = plan.workers;
+    a.n_seg = plan.n_seg;
+    a.max_live = plan.max_live;
+    a.tail = n_tail > 0 ? 1 : 0;
+    a.tail_first = n_tail - nq + 1;
+    a.tail_stride = n_tail;
+    a.seq_lens = seq_lens;
+    a.q = q;
+    a.k_new = k_tail;
+    a.v_new = v_tail;
+    a.ws_o = reinterpret_cast<float *>(reinterpret_cast<char *>(workspace) + kCounterBytes);
+    a.ws_ml = reinterpret_cast<float2 *>(reinterpret_cast<char *>(workspace) + kCounterBytes + plan.o_bytes);
+    HierArgs h;
+    h.geo = g;
+    h.B = B;
+    h.Hq = Hq;
+    h.G = a.G;
+    h.nq = nq;
+    h.max_seq_len = max_seq_len;
+    h.rows_total = plan.rows_total;
+    h.direct = plan.direct;
+    h.workers = plan.workers;
+    h.n_seg = plan.n_seg;
+    h.bt_shift = -1;
+    for (int sh = 0; sh < 31; ++sh)
+        if ((1 << sh) == g.bt) h.bt_shift = sh;
+    h.full = full ? 1 : 0;
+    h.variant = variant;
+    h.alpha = alpha;
+    h.log1p_alpha = (float)log1p((double)alpha);
+    h.seq_lens = seq_lens;
+    h.block_table = block_table;
+    h.k_plane = k_plane;
+    h.v_plane = v_plane;
+    h.meta = meta;
+    h.q = q;
+    h.ws_o = a.ws_o;
+    h.ws_ml = a.ws_ml;
+    // the merge in the same launch, under the anchor decode's rule
+    const int gp = plan.rows_total <= 4 ? 4 : plan.rows_total <= 8 ? 8 : 16;
+    h.fused = (nq == 1 && n_tail == 0 && plan.rows_total <= 16 && plan.counters_fit && plan.max_live <= 2 * (256 / gp)) ? 1 : 0;
+    h.row_chunks = plan.row_chunks;
+    h.counters = reinterpret_cast<unsigned *>(workspace);
+    h.out = out;
+    h.lse = lse;
+    hipError_t e = launch_hier_attn(h, stream);
+    if (e != hipSuccess || h.fused) return e;
+    return launch_combine(a, plan, out, lse, stream);
 }
 
 }  // namespace lynx

@@ -103,7 +103,7 @@ hipError_t launch_deserialize_residual(const Geometry &g, int b, int t0, int n,
 constexpr size_t kCounterBytes = 262144;
 constexpr int kCounterStride = 64;  // uint32 slots between counters
 constexpr int kCounters = (int)(kCounterBytes / (kCounterStride * sizeof(unsigned)));
-enum class KvMode : int { kAnchor = 0, kCodes = 1, kAnchorSplit = 2, kCodesWide = 3, kCodesHalfWide = 4 };
+enum class KvMode : int { kAnchor = 0, kCodes = 1, kAnchorSplit = 2, kCodesWide = 3, kCodesHalfWide = 4, kHier = 5 };
 
 // 128-token groups per unit of the attention kernels' work list (work_list.h):
 // one per wavefront of a workgroup.
@@ -208,6 +208,35 @@ struct SplitDecodeArgs {
 
 hipError_t launch_anchor_split_decode(const SplitDecodeArgs &args, hipStream_t stream);
 
+// Arguments of the attention over the hierarchical codec's planes (hier_attn.hip):
+// the context only; the combine kernel attends the BF16 tail.
+struct HierArgs {
+    Geometry geo;
+    int B, Hq, G, nq, max_seq_len;
+    int rows_total;    // nq * G query rows per (sequence, kv head)
+    int direct, workers, n_seg;  // as in AttnPlan
+    int bt_shift;      // log2(block_tokens) when it is a power of two, else -1
+    int full;          // merged codes instead of 4-bit planes
+    int variant;
+    float alpha, log1p_alpha;
+    const int32_t *seq_lens;
+    const int32_t *block_table;
+    const uint8_t *k_plane;
+    const uint8_t *v_plane;
+    HMetaPtrs meta;
+    const uint16_t *q;  // BF16 [B][nq][Hq][128]
+    float *ws_o;
+    float2 *ws_ml;
+    // merge in the same launch (as DecodeArgs)
+    int fused;
+    int row_chunks;
+    unsigned *counters;
+    uint16_t *out;      // BF16 [B][nq][Hq][128]
+    float *lse;         // fp32 [B][nq][Hq] or nullptr
+};
+
+hipError_t launch_hier_attn(const HierArgs &args, hipStream_t stream);
+
 // The plan of a call; its workspace is at most `most` bytes where fewer workers
 // can make it so.
 AttnPlan plan_attention(KvMode mode, const Geometry &g, int B, int Hq, int nq, int max_seq_len,
@@ -234,6 +263,16 @@ hipError_t launch_attention(KvMode mode, const Geometry &g, const AttnPlan &plan
                             const uint16_t *k_new, const uint16_t *v_new, int tail_count,
                             uint16_t *out, float *lse, void *workspace, hipStream_t stream,
                             int anchor_bits = 4);
+
+// Attention over the hierarchical codec's planes (plan_attention of KvMode::kHier):
+// the context, then where there is a tail (n_tail BF16 tokens, of which query i of
+// nq sees the first n_tail - nq + 1 + i) or the context's kernel does not merge its
+// own partials, the combine kernel.
+hipError_t launch_attn_hier(const Geometry &g, const AttnPlan &plan, int B, int Hq, int nq, int max_seq_len,
+                            const int32_t *seq_lens, const int32_t *block_table, bool full, const uint8_t *k_plane,
+                            const uint8_t *v_plane, float alpha, int variant, HMetaPtrs meta, const uint16_t *q,
+                            int n_tail, const uint16_t *k_tail, const uint16_t *v_tail, uint16_t *out, float *lse,
+                            void *workspace, hipStream_t stream);
 
 // ---- verification of a token tree (attention.hip, tree.hip) --------------------
 // Arguments of the merge of a tree's context partials with its own nodes.
@@ -297,6 +336,40 @@ struct DequantArgs {
 hipError_t launch_append(const AppendArgs &args, int B, hipStream_t stream);
 hipError_t launch_dequant(const DequantArgs &args, int B, hipStream_t stream);
 hipError_t launch_append_begin(const DequantArgs &args, int B, hipStream_t stream);
+
+// ---- norms and rotation of query and key heads (rope.hip) -----------------------
+struct RopeArgs {
+    int n_tokens, Hq, Hkv;
+    int rotary;               // dims of a head that turn, a multiple of 16
+    int pairs;                // dims 2 i and 2 i + 1 turn together, else i and i + rotary / 2
+    int n_rows;               // of the outputs
+    int64_t q_stride, k_stride, v_stride;  // elements between tokens
+    const uint16_t *q, *k, *v;             // BF16 heads of 128; v may be nullptr
+    const int32_t *positions; // [n_tokens]; negative: no token
+    const int32_t *rows;      // [n_tokens] output rows, or nullptr: row n
+    const uint16_t *q_weight, *k_weight;   // BF16 [128], or nullptr: no norm
+    float eps, scale;
+    const float *inv_freq;    // [rotary / 2]
+    uint16_t *q_out, *k_out, *v_out;
+};
+hipError_t launch_rope(const RopeArgs &args, hipStream_t stream);
+
+// ---- the plan of a step: blocks, slots, positions (blocks.hip) -------------------
+struct BlocksArgs {
+    int B, bt, max_blocks, num_blocks;
+    int capacity;             // tokens a sequence may hold
+    int n_src;                // new tokens per sequence at most
+    int max_rows;             // of the token arrays
+    const int32_t *seq_lens;  // [B]
+    const int32_t *counts;    // [B] new tokens; of a release the tokens kept
+    int32_t *block_table;     // [B][max_blocks]
+    int32_t *free_blocks;     // [num_blocks]
+    int32_t *state;           // blocks on the stack; arrivals, zero between calls
+    int32_t *granted, *starts;  // [B], [B + 1]
+    int32_t *seq_of, *positions, *slots, *rows;  // [max_rows], each may be nullptr
+};
+hipError_t launch_blocks_extend(const BlocksArgs &args, hipStream_t stream);
+hipError_t launch_blocks_release(const BlocksArgs &args, hipStream_t stream);
 
 // ---- acceptance of a token tree (spec_tree.hip) ---------------------------------
 constexpr int kTreeStateBytes = 64;

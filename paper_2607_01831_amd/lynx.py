@@ -61,7 +61,7 @@ def load():
         raise RuntimeError(f"{LIBRARY} is not built: run `python -m paper_2607_01831_amd.build` "
                            "(or __graft_entry__.build()) first")
     lib = ctypes.CDLL(str(LIBRARY))
-    P, I32, SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_size_t
+    P, I32, I64, SZ = ctypes.c_void_p, ctypes.c_int32, ctypes.c_int64, ctypes.c_size_t
     LP, MP = ctypes.POINTER(lynx_layout), ctypes.POINTER(lynx_meta)
     sigs = {
         "lynx_kv_encode": ([LP, I32, I32, P, P, P, P, P, P, P, MP, P], ctypes.c_int),
@@ -99,6 +99,12 @@ def load():
         "lynx_kv_append": ([P, I32, I32, I32, P, P, P, P, P, P, P, P, P, P, P, P, P, P, P], ctypes.c_int),
         "lynx_kv_append_begin": ([P, I32, P, P, P, P, P, P], ctypes.c_int),
         "lynx_kv_dequant": ([P, I32, I32, P, P, P, P, P, P, P, P, P], ctypes.c_int),
+        "lynx_attn_hier": ([P, I32, I32, I32, I32, P, P, I32, P, P, ctypes.c_float, I32, P, P, I32, P, P, P, P, P, SZ, P],
+                           ctypes.c_int),
+        "lynx_qk_norm_rope": ([I32, I32, I32, I32, P, I64, P, I64, P, I64, P, P, I32, P, P, ctypes.c_float, P, I32, I32,
+                               ctypes.c_float, P, P, P, P], ctypes.c_int),
+        "lynx_blocks_extend": ([P, I32, I32, I32, P, P, P, P, P, P, P, P, P, P, P, P], ctypes.c_int),
+        "lynx_blocks_release": ([P, I32, P, P, P, P, P, P], ctypes.c_int),
         "lynx_strerror": ([ctypes.c_int], ctypes.c_char_p),
     }
     for name, (args, res) in sigs.items():
@@ -685,6 +691,117 @@ def lynx_hkv_dequant(L: Layout, b: int, T: int, block_table, full: bool, k_plane
         1 if full else 0, _arg(fn, "k_plane", k_plane, plane), _arg(fn, "v_plane", v_plane, plane), alpha, variant,
         ctypes.byref(_hmeta_arg(fn, L, hmeta, b + 1)), _arg(fn, "k_out", k_out, n), _arg(fn, "v_out", v_out, n),
         _stream(stream)))
+
+
+_pack_hmeta = struct.Struct("8P").pack
+
+
+def _typed_hmeta(fn: str, L: "Layout", hmeta: "HMeta", rows: int, dev: int) -> bytes:
+    heads = rows * L.num_kv_heads
+    page, chunk = (heads * -(-L.max_tokens // n) * HEAD_DIM * 4 for n in (256, 32))
+    return _pack_hmeta(*(_typed(fn, "hmeta." + name, getattr(hmeta, name), page if name[2] == "g" else chunk, _F32, dev) or 0
+                         for name in _HMETA_NAMES))
+
+
+def lynx_attn_hier(L: Layout, B: int, Hq: int, k: int, max_seq_len: int, seq_lens, block_table, full: bool, k_plane,
+                   v_plane, alpha: float, variant: int, hmeta: HMeta, q, k_tail, v_tail, out, lse=None,
+                   workspace_buf=None, stream=None) -> None:
+    """Attention over the hierarchical codec's 4-bit planes, or its merged codes
+    (full): q [B][k][Hq][128], k_tail and v_tail [B][n_tail][Hkv][128] or None,
+    lse fp32 [B][k][Hq] or None; workspace() of k queries."""
+    fn, (dev, stream) = "lynx_attn_hier", _here(stream)
+    ws, nb, nk = workspace_buf, max(B, 0), max(k, 0)
+    if (k_tail is None) != (v_tail is None):
+        raise LynxError(fn, LYNX_EINVAL)
+    if k_tail is not None and k_tail.dim() != 4:
+        raise ValueError(f"{fn}: k_tail is [B][n_tail][Hkv][128]")
+    n_tail = 0 if k_tail is None else int(k_tail.shape[1])
+    plane, tail = L.plane_bytes(128 if full else 64), nb * n_tail * L.num_kv_heads * HEAD_DIM * 2
+    io = nb * nk * Hq * HEAD_DIM * 2
+    _check(fn, load().lynx_attn_hier(
+        _packed(L), B, Hq, k, max_seq_len, _typed(fn, "seq_lens", seq_lens, nb * 4, _I32, dev),
+        _typed(fn, "block_table", block_table, nb * L.max_blocks_per_seq * 4, _I32, dev), 1 if full else 0,
+        _typed(fn, "k_plane", k_plane, plane, _U8, dev), _typed(fn, "v_plane", v_plane, plane, _U8, dev), alpha, variant,
+        _typed_hmeta(fn, L, hmeta, nb, dev), _typed(fn, "q", q, io, _BF16, dev), n_tail,
+        _typed(fn, "k_tail", k_tail, tail, _BF16, dev), _typed(fn, "v_tail", v_tail, tail, _BF16, dev),
+        _typed(fn, "out", out, io, _BF16, dev), _typed(fn, "lse", lse, nb * nk * Hq * 4, _F32, dev),
+        _typed(fn, "workspace_buf", ws, 0, _U8, dev), 0 if ws is None else ws.nbytes, stream))
+
+
+def _heads(fn: str, what: str, t, tokens: int, dev: int):
+    """Pointer, heads and token stride of BF16 heads [tokens][heads][128], which may
+    be part of a wider row."""
+    if t is None:
+        return None, 0, 0
+    if t.dim() != 3 or t.shape[0] != tokens or t.shape[2] != HEAD_DIM:
+        raise ValueError(f"{fn}: {what} is [tokens][heads][128]")
+    heads, (step, head, one) = int(t.shape[1]), t.stride()
+    if t.dtype is not _BF16:
+        raise ValueError(f"{fn}: {what} is {t.dtype}; the call uses {_BF16}")
+    if t.get_device() != dev:
+        raise ValueError("liblynx takes device tensors" if not t.is_cuda else
+                         f"{fn}: {what} is on device {t.get_device()}, not on the current one ({dev})")
+    if one != 1 or (head != HEAD_DIM and heads > 1):
+        raise ValueError(f"{fn}: the heads of {what} do not follow one another")
+    return t.data_ptr(), heads, step if tokens > 1 else max(step, heads * HEAD_DIM) // 8 * 8
+
+
+def lynx_qk_norm_rope(q, k, v, positions, rows, q_weight, k_weight, eps: float, inv_freq, pairs: bool, scale: float,
+                      q_out, k_out, v_out, stream=None) -> None:
+    """q [tokens][Hq][128], k and v [tokens][Hkv][128] BF16, contiguous or views of
+    a fused row; positions, rows (or None) int32 [tokens]; weights BF16 [128] or
+    None; inv_freq fp32 [rotary_dim / 2] or None; q_out [rows..][Hq][128], k_out and
+    v_out [rows..][Hkv][128] (the leading dims are rows in order).  v and v_out may
+    be None."""
+    fn, (dev, stream) = "lynx_qk_norm_rope", _here(stream)
+    n = int(q.shape[0])
+    qp, Hq, qs = _heads(fn, "q", q, n, dev)
+    kp, Hkv, ks = _heads(fn, "k", k, n, dev)
+    vp, Hv, vs = _heads(fn, "v", v, n, dev)
+    if (v is None) != (v_out is None):
+        raise LynxError(fn, LYNX_EINVAL)
+    if v is not None and Hv != Hkv:
+        raise ValueError(f"{fn}: v has {Hv} heads, k {Hkv}")
+    n_rows = q_out.numel() // (Hq * HEAD_DIM) if Hq else 0
+    out = n_rows * Hkv * HEAD_DIM * 2
+    _check(fn, load().lynx_qk_norm_rope(
+        n, Hq, Hkv, HEAD_DIM, qp, qs, kp, ks, vp, vs, _typed(fn, "positions", positions, n * 4, _I32, dev),
+        _typed(fn, "rows", rows, n * 4, _I32, dev), n_rows, _typed(fn, "q_weight", q_weight, HEAD_DIM * 2, _BF16, dev),
+        _typed(fn, "k_weight", k_weight, HEAD_DIM * 2, _BF16, dev), eps, _typed(fn, "inv_freq", inv_freq, 0, _F32, dev),
+        0 if inv_freq is None else 2 * inv_freq.numel(), 1 if pairs else 0, scale,
+        _typed(fn, "q_out", q_out, 0, _BF16, dev), _typed(fn, "k_out", k_out, out, _BF16, dev),
+        _typed(fn, "v_out", v_out, out, _BF16, dev), stream))
+
+
+def _blocks_args(fn: str, L: Layout, B: int, dev: int, block_table, free_blocks, free_state):
+    return (_typed(fn, "block_table", block_table, max(B, 0) * L.max_blocks_per_seq * 4, _I32, dev),
+            _typed(fn, "free_blocks", free_blocks, L.num_blocks * 4, _I32, dev),
+            _typed(fn, "free_state", free_state, 8, _I32, dev))
+
+
+def lynx_blocks_extend(L: Layout, B: int, n_src: int, seq_lens, counts, block_table, free_blocks, free_state, granted,
+                       starts, seq_of=None, positions=None, slots=None, rows=None, stream=None) -> None:
+    """Room for counts[b] <= n_src new tokens behind every sequence; max_rows is
+    the length of the token arrays seq_of, positions, slots and rows that are given
+    (B * n_src where none is)."""
+    fn, (dev, stream) = "lynx_blocks_extend", _here(stream)
+    nb = max(B, 0)
+    given = [t.numel() for t in (seq_of, positions, slots, rows) if t is not None]
+    max_rows = min(given) if given else min(nb * max(n_src, 0), 1 << 30)
+    _check(fn, load().lynx_blocks_extend(
+        _packed(L), B, n_src, max_rows, _typed(fn, "seq_lens", seq_lens, nb * 4, _I32, dev),
+        _typed(fn, "counts", counts, nb * 4, _I32, dev), *_blocks_args(fn, L, B, dev, block_table, free_blocks, free_state),
+        _typed(fn, "granted", granted, nb * 4, _I32, dev), _typed(fn, "starts", starts, (nb + 1) * 4, _I32, dev),
+        *(_typed(fn, what, t, max_rows * 4, _I32, dev)
+          for what, t in (("seq_of", seq_of), ("positions", positions), ("slots", slots), ("rows", rows))), stream))
+
+
+def lynx_blocks_release(L: Layout, B: int, seq_lens, keep, block_table, free_blocks, free_state, stream=None) -> None:
+    fn, (dev, stream) = "lynx_blocks_release", _here(stream)
+    nb = max(B, 0)
+    _check(fn, load().lynx_blocks_release(
+        _packed(L), B, _typed(fn, "seq_lens", seq_lens, nb * 4, _I32, dev), _typed(fn, "keep", keep, nb * 4, _I32, dev),
+        *_blocks_args(fn, L, B, dev, block_table, free_blocks, free_state), stream))
 
 
 def lynx_serialized_bytes(num_kv_heads: int, n_tokens: int) -> tuple[int, int]:
