@@ -17,7 +17,11 @@ pytestmark = pytest.mark.gpu
 ALPHA = 255.0
 
 
-def test_speculative_step():
+@pytest.mark.parametrize("whole", [True, False])
+def test_speculative_step(whole, monkeypatch):
+    """whole False: the binding's own form of the calls, as where its C++ is not built."""
+    if not whole:
+        monkeypatch.setattr(lynx, "_whole", lambda *args: None)
     lens, Hq, H, bt, k, per = [300, 5, 0, 129], 8, 2, 16, 6, 24
     B, n_blocks = len(lens), 96
     L = lynx.Layout(num_kv_heads=H, block_tokens=bt, max_blocks_per_seq=per, num_blocks=n_blocks, max_tokens=per * bt)
@@ -81,3 +85,52 @@ def test_speculative_step():
         eager = out.clone()
         step()
         assert torch.equal(out, eager)
+
+
+def test_what_the_whole_calls_refuse():
+    """Device tensors that are short, of another type or strided, by the calls in C++
+    and by the binding's own form, which says what is wrong."""
+    L = lynx.Layout(num_kv_heads=2, block_tokens=16, max_blocks_per_seq=2, num_blocks=4, max_tokens=32)
+    ints = lambda *s: torch.zeros(*s, dtype=torch.int32, device="cuda")  # noqa: E731
+    b16 = lambda *s: torch.zeros(*s, dtype=torch.bfloat16, device="cuda")  # noqa: E731
+    pool, hm = lynx.KVPool.allocate(L, 2, codes=False), lynx.HMeta.empty(L, 2)
+    ws = lynx.workspace(L, 2, 4, 2, 32, tree=False)
+    attn = dict(lens=ints(2), table=ints(2, 2), kp=pool.k_anc, vp=pool.v_anc, q=b16(2, 2, 4, 128), kt=b16(2, 3, 2, 128),
+                vt=b16(2, 3, 2, 128), out=b16(2, 2, 4, 128), lse=torch.zeros(2, 2, 4, device="cuda"), ws=ws)
+    row = b16(5, 8, 128)
+    rope = dict(q=row[:, :4], k=row[:, 4:6], v=row[:, 6:], pos=ints(5), rows=ints(5), w=b16(128),
+                f=torch.zeros(64, device="cuda"), qo=b16(5, 4, 128), ko=b16(5, 2, 128), vo=b16(5, 2, 128))
+    plan = dict(lens=ints(2), counts=ints(2), table=ints(2, 2), stack=ints(4), state=ints(2), granted=ints(2), starts=ints(3),
+                pos=ints(8))
+
+    def f_attn(a):
+        lynx.lynx_attn_hier(L, 2, 4, 2, 32, a["lens"], a["table"], False, a["kp"], a["vp"], 255.0, INT4, hm, a["q"], a["kt"],
+                            a["vt"], a["out"], a["lse"], a["ws"])
+
+    def f_rope(a):
+        lynx.lynx_qk_norm_rope(a["q"], a["k"], a["v"], a["pos"], a["rows"], a["w"], a["w"], EPS, a["f"], True, 1.0, a["qo"],
+                               a["ko"], a["vo"])
+
+    def f_extend(a):
+        lynx.lynx_blocks_extend(L, 2, 4, a["lens"], a["counts"], a["table"], a["stack"], a["state"], a["granted"], a["starts"],
+                                None, a["pos"])
+
+    def f_release(a):
+        lynx.lynx_blocks_release(L, 2, a["lens"], a["counts"], a["table"], a["stack"], a["state"])
+    for f, good, names in ((f_attn, attn, attn), (f_rope, rope, rope), (f_extend, plan, plan),
+                           (f_release, plan, ("lens", "counts", "table", "stack", "state"))):
+        f(good)
+        for name in names:
+            x = good[name]
+            short = x[:, 1:] if f is f_rope and name in "qkv" else x.view(-1)[: x.numel() // 8]
+            if name in ("qo", "f"):  # (of any size: rows, rotated dims)
+                short = x.to(torch.float64)
+            if f is f_extend and name == "pos":
+                short = x.long()
+            for bad in (short, x.cpu(), x.to(torch.float16) if x.dtype != torch.float16 else x.float(),
+                        x.view(-1)[::2] if x.is_contiguous() else x[..., ::2]):
+                if f is f_rope and name == "q" and bad is short:
+                    bad = torch.cat([x, x], 1)[:, ::2]
+                with pytest.raises((ValueError, lynx.LynxError)):
+                    f({**good, name: bad})
+    torch.cuda.synchronize()
