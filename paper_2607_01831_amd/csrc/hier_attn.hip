@@ -52,11 +52,12 @@ constexpr int kPTop = 7, kSlack = 8;
 
 // LDS: the table, 64 copies of 256 entries (entry e of lane l at 256 e + 4 l, so a
 // lookup's address is the plane byte over the lane's byte, one v_perm, and every
-// lane reads a bank of its own), then a page of 16 KB: while the wavefronts attend,
-// 1 KB each for a chunk's b and m; at the end what they join.  80 KB, two
+// lane reads a bank of its own), then 16 KB: while the wavefronts attend, 1 KB each
+// for a chunk's b and m, and the queries; at the end what they join.  80 KB, two
 // workgroups per CU.
 constexpr int kTable = 256 * 256;
 constexpr int kShare = 16384;
+constexpr int kStage = 1024;
 
 __device__ __forceinline__ uint32_t pk_fma(uint32_t a, uint32_t b, uint32_t c) {
     return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(__builtin_bit_cast(f16x2_t, a),
@@ -113,21 +114,18 @@ __device__ __forceinline__ void attend_segment(const HierArgs &a, const Segment<
         return;
     }
     uint8_t *share = lds + kTable;
-    uint8_t *stage = share + w * 1024;  // K: b, m, V: b, m of a chunk, [128] fp16 each
+    uint8_t *stage = share + w * kStage;  // K: b, m, V: b, m of a chunk, [128] fp16 each
 
     // ---- where a token's rows are ----
     bool bad = false;
     const int32_t *bt_row = a.block_table + (size_t)b * a.geo.max_blocks;
+    auto block_index = [&](int t) { return LAYOUT == 0 ? 0 : a.bt_shift >= 0 ? (t >> a.bt_shift) : t / a.geo.bt; };
     auto block_row0 = [&](int t, int blk) -> size_t {  // the row of token t in its block blk
         if (blk < 0 || blk >= a.geo.num_blocks) {
             bad = true;
             blk = 0;
         }
-        const int bi = LAYOUT == 0 ? 0 : a.bt_shift >= 0 ? (t >> a.bt_shift) : t / a.geo.bt;
-        return ((size_t)blk * Hkv + h) * a.geo.bt + (size_t)(t - bi * a.geo.bt);
-    };
-    auto block_of = [&](int t) {
-        return bt_row[LAYOUT == 0 ? 0 : a.bt_shift >= 0 ? (t >> a.bt_shift) : t / a.geo.bt];
+        return ((size_t)blk * Hkv + h) * a.geo.bt + (size_t)(t - block_index(t) * a.geo.bt);
     };
 
     // ---- the wavefront's chunks ----
@@ -137,74 +135,104 @@ __device__ __forceinline__ void attend_segment(const HierArgs &a, const Segment<
     int n_mine = 4 * my_groups;
     while (n_mine > 0 && chunk_t0(n_mine - 1) >= T) --n_mine;
 
-    // ---- loads of a chunk ----
-    struct Raw {
-        uint32_t k[2][kKW];  // token 16 a + col, bytes kRow / 4 * g ..
-        uint32_t v[8][kVW];  // token slot e, dims 8 col .. + 7
-        float2 ks, km, kgs, kgm, vs, vm, vgs, vgm;  // channels 2 lane, 2 lane + 1
+    // ---- loads of a chunk: keys, values, scalars ----
+    // Past the last chunk they load that one again: every step issues as many, so a
+    // wait for one of them is no wait for those behind it.
+    uint32_t rk[2][kKW];  // token 16 i + col, bytes kRow / 4 * g ..
+    uint32_t rv[8][kVW];  // token slot e, dims 8 col .. + 7
+    float2 rm[8];         // channels 2 lane, 2 lane + 1: K's sigma, mu, gscale, gmin, V's
+    // LAYOUT 1: the blocks of a group's eight 16-token runs, run r in lane r, loaded a
+    // group ahead of the rows (entries past the table's end are clamped and unused)
+    int ids = 0, ids_next = 0;
+    auto load_ids = [&](int u) {
+        if (LAYOUT == 1)
+            ids_next = bt_row[min(block_index((seg.g0 + w + kWaves * u) * kKGroup + 16 * (lane & 7)), a.geo.max_blocks - 1)];
+    };
+    // The row's bytes of the tokens of chunk j that rows(i or e) asks for: run(i, row0)
+    // for each of its two runs of 16 tokens where they lie in one block each, else
+    // each(row_of), row_of(t) the row of token t of the chunk
+    auto rows_of_chunk = [&](int j, int run_ids, auto run, auto each) {
+        const int t0 = __builtin_amdgcn_readfirstlane(chunk_t0(j));
+        if (LAYOUT != 2 && t0 + kChunk <= T) {
+#pragma unroll
+            for (int i = 0; i < 2; ++i)
+                run(i, block_row0(t0 + 16 * i, LAYOUT == 0 ? run_ids : __builtin_amdgcn_readlane(run_ids, 2 * (j & 3) + i)) * kRow);
+        } else {
+            // a lookup per token, in lanes 0 .. 31; tokens past the context repeat the
+            // last one
+            const int t = min(t0 + (lane & 31), T - 1);
+            const size_t row = block_row0(t, bt_row[block_index(t)]) * kRow;
+            each([&](int from) -> size_t {
+                return (size_t)(uint32_t)__shfl((int)(uint32_t)row, from) | (size_t)(uint32_t)__shfl((int)(row >> 32), from) << 32;
+            });
+        }
+    };
+    auto load_k = [&](int j, int run_ids) {
+        auto put = [&](int i, const uint8_t *p) {
+#pragma unroll
+            for (int q = 0; q < kKW / 4; ++q) {
+                const uint4 u = reinterpret_cast<const uint4 *>(p)[q];
+                rk[i][4 * q] = u.x; rk[i][4 * q + 1] = u.y; rk[i][4 * q + 2] = u.z; rk[i][4 * q + 3] = u.w;
+            }
+        };
+        rows_of_chunk(j, run_ids, [&](int i, size_t row) { put(i, a.k_plane + row + (col * kRow + g * (kRow / 4))); },
+                      [&](auto row_of) {
+#pragma unroll
+                          for (int i = 0; i < 2; ++i) put(i, a.k_plane + row_of(16 * i + col) + g * (kRow / 4));
+                      });
+    };
+    auto load_v = [&](int j, int run_ids) {
+        auto put = [&](int e, const uint8_t *p) {
+            if (FULL) {
+                const uint2 u = *reinterpret_cast<const uint2 *>(p);
+                rv[e][0] = u.x;
+                rv[e][kVW - 1] = u.y;
+            } else {
+                rv[e][0] = *reinterpret_cast<const uint32_t *>(p);
+            }
+        };
+        rows_of_chunk(j, run_ids,
+                      [&](int i, size_t row) {
+#pragma unroll
+                          for (int e = 0; e < 4; ++e)
+                              put(4 * i + e, a.v_plane + row + ((4 * g + e) * kRow + col * (kRow / 16)));
+                      },
+                      [&](auto row_of) {
+#pragma unroll
+                          for (int e = 0; e < 8; ++e)
+                              put(e, a.v_plane + row_of((e < 4 ? 0 : 16) + 4 * g + (e & 3)) + col * (kRow / 16));
+                      });
     };
     const size_t cmeta = ((size_t)b * Hkv + h) * a.geo.n_chunks * kHeadDim + 2 * lane;
     const size_t pmeta = ((size_t)b * Hkv + h) * a.geo.n_pages * kHeadDim + 2 * lane;
-    auto load_k = [&](Raw &r, int i, const uint8_t *p) {
-#pragma unroll
-        for (int q = 0; q < kKW / 4; ++q) {
-            const uint4 u = reinterpret_cast<const uint4 *>(p)[q];
-            r.k[i][4 * q] = u.x; r.k[i][4 * q + 1] = u.y; r.k[i][4 * q + 2] = u.z; r.k[i][4 * q + 3] = u.w;
-        }
-    };
-    auto load_v = [&](Raw &r, int e, const uint8_t *p) {
-        if (FULL) {
-            const uint2 u = *reinterpret_cast<const uint2 *>(p);
-            r.v[e][0] = u.x;
-            r.v[e][kVW - 1] = u.y;
-        } else {
-            r.v[e][0] = *reinterpret_cast<const uint32_t *>(p);
-        }
-    };
-    auto load_chunk = [&](Raw &r, int j) {
+    auto load_meta = [&](int j) {
         const int t0 = __builtin_amdgcn_readfirstlane(chunk_t0(j));
-        {
-            const size_t c = cmeta + (size_t)(t0 / kChunk) * kHeadDim, p = pmeta + (size_t)(t0 / kPage) * kHeadDim;
-            r.ks = *reinterpret_cast<const float2 *>(a.meta.k_sigma + c);
-            r.km = *reinterpret_cast<const float2 *>(a.meta.k_mu + c);
-            r.vs = *reinterpret_cast<const float2 *>(a.meta.v_sigma + c);
-            r.vm = *reinterpret_cast<const float2 *>(a.meta.v_mu + c);
-            r.kgs = *reinterpret_cast<const float2 *>(a.meta.k_gscale + p);
-            r.kgm = *reinterpret_cast<const float2 *>(a.meta.k_gmin + p);
-            r.vgs = *reinterpret_cast<const float2 *>(a.meta.v_gscale + p);
-            r.vgm = *reinterpret_cast<const float2 *>(a.meta.v_gmin + p);
-        }
-        if (LAYOUT != 2 && t0 + kChunk <= T) {
-            // two 16-token runs, each inside one block
+        const size_t c = cmeta + (size_t)(t0 / kChunk) * kHeadDim, p = pmeta + (size_t)(t0 / kPage) * kHeadDim;
+        const float *src[8] = {a.meta.k_sigma + c, a.meta.k_mu + c, a.meta.k_gscale + p, a.meta.k_gmin + p,
+                               a.meta.v_sigma + c, a.meta.v_mu + c, a.meta.v_gscale + p, a.meta.v_gmin + p};
 #pragma unroll
-            for (int i = 0; i < 2; ++i) {
-                const int t = t0 + 16 * i;
-                const size_t row = block_row0(t, __builtin_amdgcn_readfirstlane(block_of(t))) * kRow;
-                load_k(r, i, a.k_plane + row + (col * kRow + g * (kRow / 4)));
-#pragma unroll
-                for (int e = 0; e < 4; ++e) load_v(r, 4 * i + e, a.v_plane + row + ((4 * g + e) * kRow + col * (kRow / 16)));
-            }
-        } else {
-            // a lookup per token, in lanes 0 .. 31; tokens past the context
-            // repeat the last one
-            const int t = min(t0 + (lane & 31), T - 1);
-            const size_t row = block_row0(t, block_of(t));
-            auto row_of = [&](int from) -> size_t {
-                return (size_t)(uint32_t)__shfl((int)(uint32_t)row, from) | (size_t)(uint32_t)__shfl((int)(row >> 32), from) << 32;
-            };
-#pragma unroll
-            for (int i = 0; i < 2; ++i) load_k(r, i, a.k_plane + row_of(16 * i + col) * kRow + g * (kRow / 4));
-#pragma unroll
-            for (int e = 0; e < 8; ++e)
-                load_v(r, e, a.v_plane + row_of((e < 4 ? 0 : 16) + 4 * g + (e & 3)) * kRow + col * (kRow / 16));
-        }
+        for (int i = 0; i < 8; ++i) rm[i] = *reinterpret_cast<const float2 *>(src[i]);
     };
+    const int last = n_mine - 1;
+    // the next chunk of keys; j counts up by one from 0, and the values follow it
+    auto next_k = [&](int j) {
+        if (LAYOUT == 1 && (j & 3) == 0 && j <= last) {
+            ids = ids_next;
+            load_ids(min((j >> 2) + 1, my_groups - 1));
+        }
+        load_k(min(j, last), ids);
+    };
+    if (LAYOUT == 0) ids = __builtin_amdgcn_readfirstlane(bt_row[0]);
+    if (n_mine > 0) {
+        load_meta(0);
+        load_ids(0);
+        next_k(0);
+        load_v(0, ids);
+    }
 
-    Raw raw;
-    if (n_mine > 0) load_chunk(raw, 0);
-
-    // ---- the queries as operands: row col of tile m, dims 32 g + 8 j .. + 7 ----
-    u32x4_t qf[MT][4];
+    // ---- the queries as operands, in LDS: row col of tile m, dims 32 g + 8 j .. + 7
+    // at piece 4 m + j; piece p is made by wavefront p % 4 ----
+    uint4 *s_q = reinterpret_cast<uint4 *>(share + kStage * kWaves);
     float kq[MT];  // scores in log2 units per unit of the products, without K's exponent
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
@@ -223,12 +251,15 @@ __device__ __forceinline__ void attend_segment(const HierArgs &a, const Segment<
         const float s = ldexpf(1.0f, kQTop - e_q);
         kq[m] = kLog2e * rsqrtf((float)kHeadDim) * ldexpf(1.0f, e_q - kQTop);
 #pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const uint32_t x[4] = {u[j].x, u[j].y, u[j].z, u[j].w};
-#pragma unroll
-            for (int e = 0; e < 4; ++e) qf[m][j][e] = pack_f16_rne(bf16_lo(x[e]) * s, bf16_hi(x[e]) * s);
-        }
+        for (int j = 0; j < 4; ++j)
+            if (w == j)
+                s_q[(4 * m + j) * 64 + lane] =
+                    make_uint4(pack_f16_rne(bf16_lo(u[j].x) * s, bf16_hi(u[j].x) * s),
+                               pack_f16_rne(bf16_lo(u[j].y) * s, bf16_hi(u[j].y) * s),
+                               pack_f16_rne(bf16_lo(u[j].z) * s, bf16_hi(u[j].z) * s),
+                               pack_f16_rne(bf16_lo(u[j].w) * s, bf16_hi(u[j].w) * s));
     }
+    __syncthreads();
 
     // ---- running state ----
     float m_ref[MT], l_part[MT];  // row col: the reference, the lane's share of the sum
@@ -243,79 +274,102 @@ __device__ __forceinline__ void attend_segment(const HierArgs &a, const Segment<
     int e_k = kLeast, e_v = kLeast;  // |b| + |m| < 2^e so far
 
     const uint32_t lane4 = 4u * lane;
-    // the entry of byte `by` of a word of the planes
+    // The entry of byte `by` of a word of the planes.
     auto look = [&](uint32_t word, int by) -> uint32_t {
         return *reinterpret_cast<const uint32_t *>(lds + __builtin_amdgcn_perm(word, lane4, 0x0c0c0400u + ((uint32_t)by << 8)));
     };
-
-    for (int j = 0; j < n_mine; ++j) {
-        const int t0 = __builtin_amdgcn_readfirstlane(chunk_t0(j));
-        // ---- the chunk's maps, scaled, to LDS and back in the operands' layouts ----
-        {
-            const float kb0 = raw.ks.x * raw.kgs.x, kb1 = raw.ks.y * raw.kgs.y;
-            const float km0 = fmaf(raw.km.x, raw.kgs.x, raw.kgm.x), km1 = fmaf(raw.km.y, raw.kgs.y, raw.kgm.y);
-            const float vb0 = raw.vs.x * raw.vgs.x, vb1 = raw.vs.y * raw.vgs.y;
-            const float vm0 = fmaf(raw.vm.x, raw.vgs.x, raw.vgm.x), vm1 = fmaf(raw.vm.y, raw.vgs.y, raw.vgm.y);
-            const float kt = fmaxf(fabsf(kb0) + fabsf(km0), fabsf(kb1) + fabsf(km1));
-            const float vt = fmaxf(fabsf(vb0) + fabsf(vm0), fabsf(vb1) + fabsf(vm1));
-            if (__any(kt >= ldexpf(1.0f, e_k))) e_k = max(e_k, __builtin_amdgcn_readfirstlane(exponent_of(wave_max(kt))));
-            if (__any(vt >= ldexpf(1.0f, e_v))) {
-                const int e = max(e_v, __builtin_amdgcn_readfirstlane(exponent_of(wave_max(vt))));
-                const float f = ldexpf(1.0f, max(e_v - e, -120));
+    // Lookups go in batches, each issued before the batch ahead of it is used, so their
+    // latency passes behind that one's arithmetic: a chunk's keys in kParts of them,
+    // then its values.
+    constexpr int kLooks = FULL ? 64 : 32, kBatch = MT > 1 ? 16 : 32, kParts = kLooks / kBatch;
+    uint32_t buf[2][kBatch];
+    auto look_k = [&](int part) {
 #pragma unroll
-                for (int m = 0; m < MT; ++m)
-#pragma unroll
-                    for (int n = 0; n < 8; ++n)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) o[m][n][i] *= f;
-                e_v = e;
-            }
-            const float sk = ldexpf(1.0f, kKvTop - e_k), sv = ldexpf(1.0f, kKvTop - e_v);
-            uint32_t *st = reinterpret_cast<uint32_t *>(stage) + lane;
-            st[0] = pack_f16_rne(kb0 * sk, kb1 * sk);
-            st[64] = pack_f16_rne(km0 * sk, km1 * sk);
-            st[128] = pack_f16_rne(vb0 * sv, vb1 * sv);
-            st[192] = pack_f16_rne(vm0 * sv, vm1 * sv);
+        for (int i = 0; i < kBatch; ++i) {
+            const int n = part * kBatch + i;
+            // slice n / 16, tile n / 8 % 2, byte n % 8 of its two words; or n / 8, n / 4 % 2, n % 4
+            buf[part & 1][i] = FULL ? look(rk[n >> 3 & 1][(2 * (n >> 4) + (n >> 2 & 1)) % kKW], n & 3)
+                                    : look(rk[n >> 2 & 1][(n >> 3) % kKW], n & 3);
         }
-        // ---- scores of the 32 tokens ----
-        f32x4_t sc[MT][2];
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    auto look_v = [&](int part) {
 #pragma unroll
-        for (int m = 0; m < MT; ++m) sc[m][0] = sc[m][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
-        const uint4 *kb = reinterpret_cast<const uint4 *>(stage + 64 * g);
+        for (int i = 0; i < kBatch; ++i) {
+            const int n = part * kBatch + i;  // dim n / 8, or pair of dims n / 8; token slot n % 8
+            buf[(kParts + part) & 1][i] = look(rv[n & 7][(n >> 5) % kVW], (n >> 3) & 3);
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
+    // A chunk's maps, scaled, to the wavefront's stage.
+    auto stage_maps = [&]() {
+        const float kb0 = rm[0].x * rm[2].x, kb1 = rm[0].y * rm[2].y;
+        const float km0 = fmaf(rm[1].x, rm[2].x, rm[3].x), km1 = fmaf(rm[1].y, rm[2].y, rm[3].y);
+        const float vb0 = rm[4].x * rm[6].x, vb1 = rm[4].y * rm[6].y;
+        const float vm0 = fmaf(rm[5].x, rm[6].x, rm[7].x), vm1 = fmaf(rm[5].y, rm[6].y, rm[7].y);
+        const float kt = fmaxf(fabsf(kb0) + fabsf(km0), fabsf(kb1) + fabsf(km1));
+        const float vt = fmaxf(fabsf(vb0) + fabsf(vm0), fabsf(vb1) + fabsf(vm1));
+        if (__any(kt >= ldexpf(1.0f, e_k))) e_k = max(e_k, __builtin_amdgcn_readfirstlane(exponent_of(wave_max(kt))));
+        if (__any(vt >= ldexpf(1.0f, e_v))) {
+            const int e = max(e_v, __builtin_amdgcn_readfirstlane(exponent_of(wave_max(vt))));
+            const float f = ldexpf(1.0f, max(e_v - e, -120));
 #pragma unroll
-        for (int jj = 0; jj < 4; ++jj) {
-            const uint4 bb = kb[jj], mm = kb[16 + jj];
+            for (int m = 0; m < MT; ++m)
+#pragma unroll
+                for (int n = 0; n < 8; ++n)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) o[m][n][i] *= f;
+            e_v = e;
+        }
+        const float sk = ldexpf(1.0f, kKvTop - e_k), sv = ldexpf(1.0f, kKvTop - e_v);
+        uint32_t *st = reinterpret_cast<uint32_t *>(stage) + lane;
+        st[0] = pack_f16_rne(kb0 * sk, kb1 * sk);
+        st[64] = pack_f16_rne(km0 * sk, km1 * sk);
+        st[128] = pack_f16_rne(vb0 * sv, vb1 * sv);
+        st[192] = pack_f16_rne(vm0 * sv, vm1 * sv);
+    };
+    f32x4_t sc[MT][2];
+    const uint4 *kmap = reinterpret_cast<const uint4 *>(stage + 64 * g);
+    // Scores by the slices of dims 32 g + 8 jj .. + 7 of a batch.
+    auto scores = [&](int part) {
+        const uint32_t *from = buf[part & 1];
+#pragma unroll
+        for (int s = 0; s < 4 / kParts; ++s) {
+            const int jj = 4 / kParts * part + s;
+            const uint4 bb = kmap[jj], mm = kmap[16 + jj];
             const uint32_t bw[4] = {bb.x, bb.y, bb.z, bb.w}, mw[4] = {mm.x, mm.y, mm.z, mm.w};
+            u32x4_t qf[MT];
+#pragma unroll
+            for (int m = 0; m < MT; ++m) qf[m] = reinterpret_cast<const u32x4_t *>(s_q)[(4 * m + jj) * 64 + lane];
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 u32x4_t kf;
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
-                    const uint32_t lv = FULL ? low16s(look(raw.k[i][2 * jj % kKW + e / 2], 2 * (e & 1)),
-                                                      look(raw.k[i][2 * jj % kKW + e / 2], 2 * (e & 1) + 1))
-                                             : look(raw.k[i][jj], e);
+                    const uint32_t lv = FULL ? low16s(from[(16 * s + 8 * i + 2 * e) % kBatch], from[(16 * s + 8 * i + 2 * e + 1) % kBatch])
+                                             : from[(8 * s + 4 * i + e) % kBatch];
                     kf[e] = pk_fma(lv, bw[e], mw[e]);
                 }
 #pragma unroll
-                for (int m = 0; m < MT; ++m) sc[m][i] = mfma_f16(kf, qf[m][jj], sc[m][i]);
+                for (int m = 0; m < MT; ++m) sc[m][i] = mfma_f16(kf, qf[m], sc[m][i]);
             }
         }
-        // ---- softmax weights, the second product's first operand ----
-        u32x4_t pf[MT];
+    };
+    u32x4_t pf[MT];  // softmax weights, the second product's first operand
+    auto weights = [&](int left) {  // tokens of the chunk
         const float ek = ldexpf(1.0f, e_k - kKvTop);
-        const int left = T - t0;  // tokens of the chunk
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
-            float x[8];
+            float z[8];
             const float s = kq[m] * ek;
 #pragma unroll
-            for (int e = 0; e < 8; ++e) x[e] = sc[m][e >> 2][e & 3] * s;
+            for (int e = 0; e < 8; ++e) z[e] = sc[m][e >> 2][e & 3] * s;
             if (left < kChunk) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
-                    if ((e < 4 ? 0 : 16) + 4 * g + (e & 3) >= left) x[e] = -INFINITY;
+                    if ((e < 4 ? 0 : 16) + 4 * g + (e & 3) >= left) z[e] = -INFINITY;
             }
-            const float top = max_kg(fmax3(fmax3(x[0], x[1], x[2]), fmax3(x[3], x[4], x[5]), fmax2(x[6], x[7])));
+            const float top = max_kg(fmax3(fmax3(z[0], z[1], z[2]), fmax3(z[3], z[4], z[5]), fmax2(z[6], z[7])));
             if (__any(top > m_ref[m] + (float)kSlack)) {
                 const float next = fmax2(m_ref[m], top);
                 const float f = m_ref[m] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_ref[m] - next);
@@ -330,42 +384,82 @@ __device__ __forceinline__ void attend_segment(const HierArgs &a, const Segment<
                     for (int i = 0; i < 4; ++i) o[m][n][i] *= fr[i];
             }
             const float off = m_ref[m] - (float)kPTop;
-            float p[8];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) p[e] = __builtin_amdgcn_exp2f(x[e] - off);
-            l_part[m] += ((p[0] + p[1]) + (p[2] + p[3])) + ((p[4] + p[5]) + (p[6] + p[7]));
+            for (int e = 0; e < 8; ++e) z[e] = __builtin_amdgcn_exp2f(z[e] - off);
+            l_part[m] += ((z[0] + z[1]) + (z[2] + z[3])) + ((z[4] + z[5]) + (z[6] + z[7]));
 #pragma unroll
-            for (int e = 0; e < 4; ++e) pf[m][e] = pack_f16_rne(p[2 * e], p[2 * e + 1]);
+            for (int e = 0; e < 4; ++e) pf[m][e] = pack_f16_rne(z[2 * e], z[2 * e + 1]);
         }
-        // ---- weights times values ----
-        {
-            const uint4 bb = reinterpret_cast<const uint4 *>(stage + 512)[col];
-            const uint4 mm = reinterpret_cast<const uint4 *>(stage + 768)[col];
-            const uint32_t bw[4] = {bb.x, bb.y, bb.z, bb.w}, mw[4] = {mm.x, mm.y, mm.z, mm.w};
+    };
+    // Weights times the values of a batch: operands of dim 8 col + n hold slots 2 d, 2 d + 1.
+    auto values = [&](int part, const uint32_t *bw, const uint32_t *mw) {
+        const uint32_t *from = buf[(kParts + part) & 1];
 #pragma unroll
-            for (int n2 = 0; n2 < 4; ++n2) {  // dims 8 col + 2 n2, + 1
-                uint32_t x[8];
+        for (int s = 0; s < kBatch / 8; ++s) {
+            const int n = kBatch / 8 * part + s;
+            if (FULL) {
+                u32x4_t v;
+                const uint32_t b1 = n & 1 ? high16s(bw[n >> 1 & 3], bw[n >> 1 & 3]) : low16s(bw[n >> 1 & 3], bw[n >> 1 & 3]);
+                const uint32_t m1 = n & 1 ? high16s(mw[n >> 1 & 3], mw[n >> 1 & 3]) : low16s(mw[n >> 1 & 3], mw[n >> 1 & 3]);
 #pragma unroll
-                for (int e = 0; e < 8; ++e) {
-                    const uint32_t lv = FULL ? low16s(look(raw.v[e][n2 / 2 % kVW], 2 * (n2 & 1)),
-                                                      look(raw.v[e][n2 / 2 % kVW], 2 * (n2 & 1) + 1))
-                                             : look(raw.v[e][0], n2);
-                    x[e] = pk_fma(lv, bw[n2], mw[n2]);
-                }
+                for (int d = 0; d < 4; ++d) v[d] = pk_fma(low16s(from[8 * s + 2 * d], from[8 * s + 2 * d + 1]), b1, m1);
+#pragma unroll
+                for (int m = 0; m < MT; ++m) o[m][n & 7] = mfma_f16(pf[m], v, o[m][n & 7]);
+            } else {
+                uint32_t v[8];
+#pragma unroll
+                for (int e = 0; e < 8; ++e) v[e] = pk_fma(from[8 * s + e], bw[n & 3], mw[n & 3]);
                 u32x4_t lo, hi;
 #pragma unroll
                 for (int d = 0; d < 4; ++d) {
-                    lo[d] = low16s(x[2 * d], x[2 * d + 1]);
-                    hi[d] = high16s(x[2 * d], x[2 * d + 1]);
+                    lo[d] = low16s(v[2 * d], v[2 * d + 1]);
+                    hi[d] = high16s(v[2 * d], v[2 * d + 1]);
                 }
 #pragma unroll
                 for (int m = 0; m < MT; ++m) {
-                    o[m][2 * n2] = mfma_f16(pf[m], lo, o[m][2 * n2]);
-                    o[m][2 * n2 + 1] = mfma_f16(pf[m], hi, o[m][2 * n2 + 1]);
+                    o[m][2 * n & 7] = mfma_f16(pf[m], lo, o[m][2 * n & 7]);
+                    o[m][(2 * n + 1) & 7] = mfma_f16(pf[m], hi, o[m][(2 * n + 1) & 7]);
                 }
             }
         }
-        if (j + 1 < n_mine) load_chunk(raw, j + 1);
+    };
+    if (n_mine > 0) {
+        stage_maps();
+        load_meta(min(1, last));
+        look_k(0);
+        if (kParts == 1) next_k(1);
+    }
+    for (int j = 0; j < n_mine; ++j) {
+#pragma unroll
+        for (int m = 0; m < MT; ++m) sc[m][0] = sc[m][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
+#pragma unroll
+        for (int part = 0; part < kParts; ++part) {
+            if (part + 1 < kParts) {
+                look_k(part + 1);
+                if (part + 2 == kParts) next_k(j + 1);
+            } else {
+                look_v(0);
+                if (kParts == 1) load_v(min(j + 1, last), ids);
+            }
+            scores(part);
+        }
+        const uint4 bb = reinterpret_cast<const uint4 *>(stage + 512)[col];
+        const uint4 mm = reinterpret_cast<const uint4 *>(stage + 768)[col];
+        const uint32_t bw[4] = {bb.x, bb.y, bb.z, bb.w}, mw[4] = {mm.x, mm.y, mm.z, mm.w};
+        weights(T - chunk_t0(j));
+#pragma unroll
+        for (int part = 0; part < kParts; ++part) {
+            if (part + 1 < kParts) {
+                look_v(part + 1);
+                if (part + 2 == kParts) load_v(min(j + 1, last), ids);
+            } else {
+                look_k(0);
+                if (kParts == 1) next_k(j + 2);
+            }
+            values(part, bw, mw);
+        }
+        stage_maps();
+        load_meta(min(j + 2, last));
     }
 
     // ---- the wavefronts meet: (max, sum) of every row, then the outputs ----
