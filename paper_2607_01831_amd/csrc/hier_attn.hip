@@ -25,7 +25,7 @@
 // each that brings the largest |b| + |m| so far below 2^14, so values 2^-28 of the
 // largest lose bits; a query row by its largest element.
 #include "f16_ops.h"
-#include "hier_levels.h"
+#include "hier_ops.h"
 #include "lane_ops.h"
 #include "lynx_internal.h"
 #include "split_merge.h"
@@ -40,37 +40,12 @@ namespace {
 
 constexpr int kThreads = 256;
 constexpr int kWaves = 4;
-constexpr int kChunk = 32;   // tokens of a codec chunk, and of a wavefront's step
-constexpr int kPage = 256;   // tokens of a codec page
+constexpr int kChunk = kHierChunk;  // tokens of a wavefront's step
 constexpr float kLog2e = 1.4426950408889634f;
-// The largest |b| + |m| of the scaled K and V, and the largest |q|: products up to
-// 2^24, sums in fp32.
-constexpr int kKvTop = 14, kQTop = 10;
-// A softmax weight is exp2(score - reference + kPTop); the reference moves when a
-// score passes it by kSlack, so weights stay below 2^(kPTop + kSlack) < 65504.
-constexpr int kPTop = 7, kSlack = 8;
 
-// LDS: the table, 64 copies of 256 entries (entry e of lane l at 256 e + 4 l, so a
-// lookup's address is the plane byte over the lane's byte, one v_perm, and every
-// lane reads a bank of its own), then 16 KB: while the wavefronts attend, 1 KB each
-// for a chunk's b and m, and the queries; at the end what they join.  80 KB, two
-// workgroups per CU.
-constexpr int kTable = 256 * 256;
+// LDS: the table, then 16 KB: while the wavefronts attend, a stage each for a chunk's
+// maps, and the queries; at the end what they join.  80 KB, two workgroups per CU.
 constexpr int kShare = 16384;
-constexpr int kStage = 1024;
-
-__device__ __forceinline__ uint32_t pk_fma(uint32_t a, uint32_t b, uint32_t c) {
-    return __builtin_bit_cast(uint32_t, __builtin_elementwise_fma(__builtin_bit_cast(f16x2_t, a),
-                                                                  __builtin_bit_cast(f16x2_t, b),
-                                                                  __builtin_bit_cast(f16x2_t, c)));
-}
-__device__ __forceinline__ uint32_t low16s(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x05040100u); }
-__device__ __forceinline__ uint32_t high16s(uint32_t a, uint32_t b) { return __builtin_amdgcn_perm(b, a, 0x07060302u); }
-// Largest of a non-negative value over the wavefront, uniform; a NaN may be lost.
-__device__ __forceinline__ float wave_max(float v) { return row_max<64>(v); }
-// The exponent e with x < 2^e (x >= 0), kept where 2^(kKvTop - e) is a normal float.
-constexpr int kLeast = -112;
-__device__ __forceinline__ int exponent_of(float x) { return max((int)(__float_as_uint(x) >> 23) - 126, kLeast); }
 
 // One segment of a worker's share, kv head h, rows r0 .. r0 + 16 MT - 1.
 // Wavefront w owns the 128-token groups w, w + 4, ... of the segment and attends
@@ -84,7 +59,8 @@ __device__ __forceinline__ int exponent_of(float x) { return max((int)(__float_a
 // tile of 16 columns, so an output lane holds dims 8 col .. + 7 of rows 4 g + i.
 //
 // LAYOUT 0: one block per sequence; 1: block_tokens a multiple of 16; 2: any other.
-template <int MT, int FULL, int LAYOUT>
+// FILL: the table is still to be made.
+template <int MT, int FULL, int LAYOUT, bool FILL>
 __device__ __forceinline__ void attend_segment(const HierArgs &a, const Segment<kWorkUnit> &seg, int h, int chunk_rows,
                                                const int tid, uint8_t *lds) {
     static_assert(kWorkUnit == kWaves, "a group per wavefront and unit");
@@ -113,8 +89,8 @@ __device__ __forceinline__ void attend_segment(const HierArgs &a, const Segment<
         }
         return;
     }
-    uint8_t *share = lds + kTable;
-    uint8_t *stage = share + w * kStage;  // K: b, m, V: b, m of a chunk, [128] fp16 each
+    uint8_t *share = lds + kTableBytes;
+    uint8_t *stage = share + w * kStageBytes;  // K: b, m, V: b, m of a chunk, [128] fp16 each
 
     // ---- where a token's rows are ----
     bool bad = false;
@@ -167,6 +143,8 @@ __device__ __forceinline__ void attend_segment(const HierArgs &a, const Segment<
             });
         }
     };
+    // (unsigned 32-bit lane offsets from uniform bases: a load then takes no arithmetic)
+    const uint32_t k_off = col * kRow + g * (kRow / 4), v_off = 4 * g * kRow + col * (kRow / 16), m_off = 2 * lane;
     auto load_k = [&](int j, int run_ids) {
         auto put = [&](int i, const uint8_t *p) {
 #pragma unroll
@@ -175,10 +153,10 @@ __device__ __forceinline__ void attend_segment(const HierArgs &a, const Segment<
                 rk[i][4 * q] = u.x; rk[i][4 * q + 1] = u.y; rk[i][4 * q + 2] = u.z; rk[i][4 * q + 3] = u.w;
             }
         };
-        rows_of_chunk(j, run_ids, [&](int i, size_t row) { put(i, a.k_plane + row + (col * kRow + g * (kRow / 4))); },
+        rows_of_chunk(j, run_ids, [&](int i, size_t row) { put(i, a.k_plane + row + k_off); },
                       [&](auto row_of) {
 #pragma unroll
-                          for (int i = 0; i < 2; ++i) put(i, a.k_plane + row_of(16 * i + col) + g * (kRow / 4));
+                          for (int i = 0; i < 2; ++i) put(i, a.k_plane + row_of(16 * i + col) + (uint32_t)(g * (kRow / 4)));
                       });
     };
     auto load_v = [&](int j, int run_ids) {
@@ -195,7 +173,7 @@ __device__ __forceinline__ void attend_segment(const HierArgs &a, const Segment<
                       [&](int i, size_t row) {
 #pragma unroll
                           for (int e = 0; e < 4; ++e)
-                              put(4 * i + e, a.v_plane + row + ((4 * g + e) * kRow + col * (kRow / 16)));
+                              put(4 * i + e, a.v_plane + row + e * kRow + v_off);
                       },
                       [&](auto row_of) {
 #pragma unroll
@@ -203,15 +181,15 @@ __device__ __forceinline__ void attend_segment(const HierArgs &a, const Segment<
                               put(e, a.v_plane + row_of((e < 4 ? 0 : 16) + 4 * g + (e & 3)) + col * (kRow / 16));
                       });
     };
-    const size_t cmeta = ((size_t)b * Hkv + h) * a.geo.n_chunks * kHeadDim + 2 * lane;
-    const size_t pmeta = ((size_t)b * Hkv + h) * a.geo.n_pages * kHeadDim + 2 * lane;
+    const size_t cmeta = ((size_t)b * Hkv + h) * a.geo.n_chunks * kHeadDim;
+    const size_t pmeta = ((size_t)b * Hkv + h) * a.geo.n_pages * kHeadDim;
     auto load_meta = [&](int j) {
         const int t0 = __builtin_amdgcn_readfirstlane(chunk_t0(j));
-        const size_t c = cmeta + (size_t)(t0 / kChunk) * kHeadDim, p = pmeta + (size_t)(t0 / kPage) * kHeadDim;
+        const size_t c = cmeta + (size_t)(t0 / kChunk) * kHeadDim, p = pmeta + (size_t)(t0 / kHierPage) * kHeadDim;
         const float *src[8] = {a.meta.k_sigma + c, a.meta.k_mu + c, a.meta.k_gscale + p, a.meta.k_gmin + p,
                                a.meta.v_sigma + c, a.meta.v_mu + c, a.meta.v_gscale + p, a.meta.v_gmin + p};
 #pragma unroll
-        for (int i = 0; i < 8; ++i) rm[i] = *reinterpret_cast<const float2 *>(src[i]);
+        for (int i = 0; i < 8; ++i) rm[i] = *reinterpret_cast<const float2 *>(src[i] + m_off);
     };
     const int last = n_mine - 1;
     // the next chunk of keys; j counts up by one from 0, and the values follow it
@@ -230,9 +208,11 @@ __device__ __forceinline__ void attend_segment(const HierArgs &a, const Segment<
         load_v(0, ids);
     }
 
+    if (FILL) fill_table<FULL>(a, lds);  // (the first rows are on their way)
+
     // ---- the queries as operands, in LDS: row col of tile m, dims 32 g + 8 j .. + 7
     // at piece 4 m + j; piece p is made by wavefront p % 4 ----
-    uint4 *s_q = reinterpret_cast<uint4 *>(share + kStage * kWaves);
+    u32x4_t *s_q = reinterpret_cast<u32x4_t *>(share + kStageBytes * kWaves);
     float kq[MT];  // scores in log2 units per unit of the products, without K's exponent
 #pragma unroll
     for (int m = 0; m < MT; ++m) {
@@ -254,10 +234,10 @@ __device__ __forceinline__ void attend_segment(const HierArgs &a, const Segment<
         for (int j = 0; j < 4; ++j)
             if (w == j)
                 s_q[(4 * m + j) * 64 + lane] =
-                    make_uint4(pack_f16_rne(bf16_lo(u[j].x) * s, bf16_hi(u[j].x) * s),
-                               pack_f16_rne(bf16_lo(u[j].y) * s, bf16_hi(u[j].y) * s),
-                               pack_f16_rne(bf16_lo(u[j].z) * s, bf16_hi(u[j].z) * s),
-                               pack_f16_rne(bf16_lo(u[j].w) * s, bf16_hi(u[j].w) * s));
+                    u32x4_t{pack_f16_rne(bf16_lo(u[j].x) * s, bf16_hi(u[j].x) * s),
+                            pack_f16_rne(bf16_lo(u[j].y) * s, bf16_hi(u[j].y) * s),
+                            pack_f16_rne(bf16_lo(u[j].z) * s, bf16_hi(u[j].z) * s),
+                            pack_f16_rne(bf16_lo(u[j].w) * s, bf16_hi(u[j].w) * s)};
     }
     __syncthreads();
 
@@ -272,16 +252,14 @@ __device__ __forceinline__ void attend_segment(const HierArgs &a, const Segment<
         for (int n = 0; n < 8; ++n) o[m][n] = f32x4_t{0.f, 0.f, 0.f, 0.f};
     }
     int e_k = kLeast, e_v = kLeast;  // |b| + |m| < 2^e so far
+    float k_lim = ldexpf(1.0f, kLeast), v_lim = k_lim;  // 2^e
 
     const uint32_t lane4 = 4u * lane;
-    // The entry of byte `by` of a word of the planes.
-    auto look = [&](uint32_t word, int by) -> uint32_t {
-        return *reinterpret_cast<const uint32_t *>(lds + __builtin_amdgcn_perm(word, lane4, 0x0c0c0400u + ((uint32_t)by << 8)));
-    };
+    auto look = [&](uint32_t word, int by) { return look_up(lds, word, by, lane4); };
     // Lookups go in batches, each issued before the batch ahead of it is used, so their
     // latency passes behind that one's arithmetic: a chunk's keys in kParts of them,
     // then its values.
-    constexpr int kLooks = FULL ? 64 : 32, kBatch = MT > 1 ? 16 : 32, kParts = kLooks / kBatch;
+    constexpr int kLooks = FULL ? 64 : 32, kBatch = 16, kParts = kLooks / kBatch;
     uint32_t buf[2][kBatch];
     auto look_k = [&](int part) {
 #pragma unroll
@@ -294,24 +272,34 @@ __device__ __forceinline__ void attend_segment(const HierArgs &a, const Segment<
         __builtin_amdgcn_sched_barrier(0);
     };
     auto look_v = [&](int part) {
+        if (!FULL && part == 0) {
+            // two tokens' words of 8 dims become the even dims' and the odd dims' of both:
+            // a byte, looked up, is then the operand's pair of token slots
+#pragma unroll
+            for (int e = 0; e < 8; e += 2) {
+                const uint32_t x = rv[e][0], y = rv[e + 1][0];
+                rv[e][0] = (x & 0x0F0F0F0Fu) | ((y << 4) & 0xF0F0F0F0u);
+                rv[e + 1][0] = ((x >> 4) & 0x0F0F0F0Fu) | (y & 0xF0F0F0F0u);
+            }
+        }
 #pragma unroll
         for (int i = 0; i < kBatch; ++i) {
-            const int n = part * kBatch + i;  // dim n / 8, or pair of dims n / 8; token slot n % 8
-            buf[(kParts + part) & 1][i] = look(rv[n & 7][(n >> 5) % kVW], (n >> 3) & 3);
+            const int n = part * kBatch + i;
+            // dim n / 8, token slot n % 8; or the pair of slots 2 (n % 4), + 1 of dim n / 4
+            buf[(kParts + part) & 1][i] = FULL ? look(rv[n & 7][(n >> 5) % kVW], (n >> 3) & 3)
+                                               : look(rv[2 * (n & 3) + (n >> 2 & 1)][0], n >> 3);
         }
         __builtin_amdgcn_sched_barrier(0);
     };
     // A chunk's maps, scaled, to the wavefront's stage.
-    auto stage_maps = [&]() {
-        const float kb0 = rm[0].x * rm[2].x, kb1 = rm[0].y * rm[2].y;
-        const float km0 = fmaf(rm[1].x, rm[2].x, rm[3].x), km1 = fmaf(rm[1].y, rm[2].y, rm[3].y);
-        const float vb0 = rm[4].x * rm[6].x, vb1 = rm[4].y * rm[6].y;
-        const float vm0 = fmaf(rm[5].x, rm[6].x, rm[7].x), vm1 = fmaf(rm[5].y, rm[6].y, rm[7].y);
-        const float kt = fmaxf(fabsf(kb0) + fabsf(km0), fabsf(kb1) + fabsf(km1));
-        const float vt = fmaxf(fabsf(vb0) + fabsf(vm0), fabsf(vb1) + fabsf(vm1));
-        if (__any(kt >= ldexpf(1.0f, e_k))) e_k = max(e_k, __builtin_amdgcn_readfirstlane(exponent_of(wave_max(kt))));
-        if (__any(vt >= ldexpf(1.0f, e_v))) {
-            const int e = max(e_v, __builtin_amdgcn_readfirstlane(exponent_of(wave_max(vt))));
+    auto next_maps = [&]() {
+        const Maps x = maps_of(rm);
+        if (__any(x.k_top >= k_lim)) {
+            e_k = max(e_k, __builtin_amdgcn_readfirstlane(exponent_of(wave_max(x.k_top))));
+            k_lim = ldexpf(1.0f, e_k);
+        }
+        if (__any(x.v_top >= v_lim)) {
+            const int e = max(e_v, __builtin_amdgcn_readfirstlane(exponent_of(wave_max(x.v_top))));
             const float f = ldexpf(1.0f, max(e_v - e, -120));
 #pragma unroll
             for (int m = 0; m < MT; ++m)
@@ -320,27 +308,31 @@ __device__ __forceinline__ void attend_segment(const HierArgs &a, const Segment<
 #pragma unroll
                     for (int i = 0; i < 4; ++i) o[m][n][i] *= f;
             e_v = e;
+            v_lim = ldexpf(1.0f, e_v);
         }
-        const float sk = ldexpf(1.0f, kKvTop - e_k), sv = ldexpf(1.0f, kKvTop - e_v);
-        uint32_t *st = reinterpret_cast<uint32_t *>(stage) + lane;
-        st[0] = pack_f16_rne(kb0 * sk, kb1 * sk);
-        st[64] = pack_f16_rne(km0 * sk, km1 * sk);
-        st[128] = pack_f16_rne(vb0 * sv, vb1 * sv);
-        st[192] = pack_f16_rne(vm0 * sv, vm1 * sv);
+        stage_maps(x, e_k, e_v, lane, stage);
     };
     f32x4_t sc[MT][2];
-    const uint4 *kmap = reinterpret_cast<const uint4 *>(stage + 64 * g);
+    const u32x4_t *kmap = reinterpret_cast<const u32x4_t *>(stage + 64 * g);
+    // What a batch of keys meets: its slices' maps and queries.  They are read ahead of
+    // the lookups of the batch behind it: LDS answers in order.
+    constexpr int kSlices = 4 / kParts;
+    u32x4_t kb[kSlices], km[kSlices], qf[kSlices][MT];
+    auto read_k = [&](int part) {
+#pragma unroll
+        for (int s = 0; s < kSlices; ++s) {
+            kb[s] = kmap[kSlices * part + s];
+            km[s] = kmap[16 + kSlices * part + s];
+#pragma unroll
+            for (int m = 0; m < MT; ++m) qf[s][m] = s_q[(4 * m + kSlices * part + s) * 64 + lane];
+        }
+        __builtin_amdgcn_sched_barrier(0);
+    };
     // Scores by the slices of dims 32 g + 8 jj .. + 7 of a batch.
     auto scores = [&](int part) {
         const uint32_t *from = buf[part & 1];
 #pragma unroll
-        for (int s = 0; s < 4 / kParts; ++s) {
-            const int jj = 4 / kParts * part + s;
-            const uint4 bb = kmap[jj], mm = kmap[16 + jj];
-            const uint32_t bw[4] = {bb.x, bb.y, bb.z, bb.w}, mw[4] = {mm.x, mm.y, mm.z, mm.w};
-            u32x4_t qf[MT];
-#pragma unroll
-            for (int m = 0; m < MT; ++m) qf[m] = reinterpret_cast<const u32x4_t *>(s_q)[(4 * m + jj) * 64 + lane];
+        for (int s = 0; s < kSlices; ++s) {
 #pragma unroll
             for (int i = 0; i < 2; ++i) {
                 u32x4_t kf;
@@ -348,10 +340,10 @@ __device__ __forceinline__ void attend_segment(const HierArgs &a, const Segment<
                 for (int e = 0; e < 4; ++e) {
                     const uint32_t lv = FULL ? low16s(from[(16 * s + 8 * i + 2 * e) % kBatch], from[(16 * s + 8 * i + 2 * e + 1) % kBatch])
                                              : from[(8 * s + 4 * i + e) % kBatch];
-                    kf[e] = pk_fma(lv, bw[e], mw[e]);
+                    kf[e] = pk_fma(lv, kb[s][e], km[s][e]);
                 }
 #pragma unroll
-                for (int m = 0; m < MT; ++m) sc[m][i] = mfma_f16(kf, qf[m], sc[m][i]);
+                for (int m = 0; m < MT; ++m) sc[m][i] = mfma_f16(kf, qf[s][m], sc[m][i]);
             }
         }
     };
@@ -361,15 +353,15 @@ __device__ __forceinline__ void attend_segment(const HierArgs &a, const Segment<
 #pragma unroll
         for (int m = 0; m < MT; ++m) {
             float z[8];
-            const float s = kq[m] * ek;
+            const float s = fmaxf(kq[m] * ek, FLT_MIN);  // (0 would not mask)
 #pragma unroll
-            for (int e = 0; e < 8; ++e) z[e] = sc[m][e >> 2][e & 3] * s;
+            for (int e = 0; e < 8; ++e) z[e] = sc[m][e >> 2][e & 3];
             if (left < kChunk) {
 #pragma unroll
                 for (int e = 0; e < 8; ++e)
                     if ((e < 4 ? 0 : 16) + 4 * g + (e & 3) >= left) z[e] = -INFINITY;
             }
-            const float top = max_kg(fmax3(fmax3(z[0], z[1], z[2]), fmax3(z[3], z[4], z[5]), fmax2(z[6], z[7])));
+            const float top = max_kg(fmax3(fmax3(z[0], z[1], z[2]), fmax3(z[3], z[4], z[5]), fmax2(z[6], z[7]))) * s;
             if (__any(top > m_ref[m] + (float)kSlack)) {
                 const float next = fmax2(m_ref[m], top);
                 const float f = m_ref[m] == -INFINITY ? 0.0f : __builtin_amdgcn_exp2f(m_ref[m] - next);
@@ -383,48 +375,36 @@ __device__ __forceinline__ void attend_segment(const HierArgs &a, const Segment<
 #pragma unroll
                     for (int i = 0; i < 4; ++i) o[m][n][i] *= fr[i];
             }
-            const float off = m_ref[m] - (float)kPTop;
+            const float off = (float)kPTop - m_ref[m];
 #pragma unroll
-            for (int e = 0; e < 8; ++e) z[e] = __builtin_amdgcn_exp2f(z[e] - off);
+            for (int e = 0; e < 8; ++e) z[e] = __builtin_amdgcn_exp2f(fmaf(z[e], s, off));
             l_part[m] += ((z[0] + z[1]) + (z[2] + z[3])) + ((z[4] + z[5]) + (z[6] + z[7]));
 #pragma unroll
             for (int e = 0; e < 4; ++e) pf[m][e] = pack_f16_rne(z[2 * e], z[2 * e + 1]);
         }
     };
     // Weights times the values of a batch: operands of dim 8 col + n hold slots 2 d, 2 d + 1.
-    auto values = [&](int part, const uint32_t *bw, const uint32_t *mw) {
+    u32x4_t bw, mw;  // the maps of dims 8 col .. + 7
+    auto values = [&](int part) {
         const uint32_t *from = buf[(kParts + part) & 1];
+        constexpr int kPer = 8 / kParts;
 #pragma unroll
-        for (int s = 0; s < kBatch / 8; ++s) {
-            const int n = kBatch / 8 * part + s;
-            if (FULL) {
-                u32x4_t v;
-                const uint32_t b1 = n & 1 ? high16s(bw[n >> 1 & 3], bw[n >> 1 & 3]) : low16s(bw[n >> 1 & 3], bw[n >> 1 & 3]);
-                const uint32_t m1 = n & 1 ? high16s(mw[n >> 1 & 3], mw[n >> 1 & 3]) : low16s(mw[n >> 1 & 3], mw[n >> 1 & 3]);
+        for (int s = 0; s < kPer; ++s) {
+            const int n = kPer * part + s;
+            u32x4_t v;
+            const uint32_t b1 = n & 1 ? high16s(bw[n >> 1 & 3], bw[n >> 1 & 3]) : low16s(bw[n >> 1 & 3], bw[n >> 1 & 3]);
+            const uint32_t m1 = n & 1 ? high16s(mw[n >> 1 & 3], mw[n >> 1 & 3]) : low16s(mw[n >> 1 & 3], mw[n >> 1 & 3]);
 #pragma unroll
-                for (int d = 0; d < 4; ++d) v[d] = pk_fma(low16s(from[8 * s + 2 * d], from[8 * s + 2 * d + 1]), b1, m1);
+            for (int d = 0; d < 4; ++d)
+                v[d] = pk_fma(FULL ? low16s(from[(8 * s + 2 * d) % kBatch], from[(8 * s + 2 * d + 1) % kBatch])
+                                   : from[(4 * s + d) % kBatch],
+                              b1, m1);
 #pragma unroll
-                for (int m = 0; m < MT; ++m) o[m][n & 7] = mfma_f16(pf[m], v, o[m][n & 7]);
-            } else {
-                uint32_t v[8];
-#pragma unroll
-                for (int e = 0; e < 8; ++e) v[e] = pk_fma(from[8 * s + e], bw[n & 3], mw[n & 3]);
-                u32x4_t lo, hi;
-#pragma unroll
-                for (int d = 0; d < 4; ++d) {
-                    lo[d] = low16s(v[2 * d], v[2 * d + 1]);
-                    hi[d] = high16s(v[2 * d], v[2 * d + 1]);
-                }
-#pragma unroll
-                for (int m = 0; m < MT; ++m) {
-                    o[m][2 * n & 7] = mfma_f16(pf[m], lo, o[m][2 * n & 7]);
-                    o[m][(2 * n + 1) & 7] = mfma_f16(pf[m], hi, o[m][(2 * n + 1) & 7]);
-                }
-            }
+            for (int m = 0; m < MT; ++m) o[m][n & 7] = mfma_f16(pf[m], v, o[m][n & 7]);
         }
     };
     if (n_mine > 0) {
-        stage_maps();
+        next_maps();
         load_meta(min(1, last));
         look_k(0);
         if (kParts == 1) next_k(1);
@@ -434,6 +414,7 @@ __device__ __forceinline__ void attend_segment(const HierArgs &a, const Segment<
         for (int m = 0; m < MT; ++m) sc[m][0] = sc[m][1] = f32x4_t{0.f, 0.f, 0.f, 0.f};
 #pragma unroll
         for (int part = 0; part < kParts; ++part) {
+            read_k(part);
             if (part + 1 < kParts) {
                 look_k(part + 1);
                 if (part + 2 == kParts) next_k(j + 1);
@@ -443,9 +424,8 @@ __device__ __forceinline__ void attend_segment(const HierArgs &a, const Segment<
             }
             scores(part);
         }
-        const uint4 bb = reinterpret_cast<const uint4 *>(stage + 512)[col];
-        const uint4 mm = reinterpret_cast<const uint4 *>(stage + 768)[col];
-        const uint32_t bw[4] = {bb.x, bb.y, bb.z, bb.w}, mw[4] = {mm.x, mm.y, mm.z, mm.w};
+        bw = reinterpret_cast<const u32x4_t *>(stage + 512)[col];
+        mw = reinterpret_cast<const u32x4_t *>(stage + 768)[col];
         weights(T - chunk_t0(j));
 #pragma unroll
         for (int part = 0; part < kParts; ++part) {
@@ -456,9 +436,9 @@ __device__ __forceinline__ void attend_segment(const HierArgs &a, const Segment<
                 look_k(0);
                 if (kParts == 1) next_k(j + 2);
             }
-            values(part, bw, mw);
+            values(part);
         }
-        stage_maps();
+        next_maps();
         load_meta(min(j + 2, last));
     }
 
@@ -551,49 +531,26 @@ __device__ __forceinline__ void attend_segment(const HierArgs &a, const Segment<
     }
 }
 
-// The table's entry of every plane byte, in 64 copies.
-template <int FULL>
-__device__ __forceinline__ void fill_table(const HierArgs &a, uint8_t *lds) {
-    const int tid = threadIdx.x;
-    // the thread's byte, its entry, then rows of 64 copies, 16 bytes a lane
-    uint32_t entry;
-    if (FULL) {
-        const uint32_t x = __builtin_bit_cast(uint16_t, signed_level_f16<1>(a.alpha, a.log1p_alpha, a.variant, tid >> 4, tid & 15));
-        entry = x | x << 16;
-    } else {
-        entry = __builtin_bit_cast(uint16_t, signed_level_f16<0>(a.alpha, a.log1p_alpha, a.variant, tid & 15, 0)) |
-                (uint32_t)__builtin_bit_cast(uint16_t, signed_level_f16<0>(a.alpha, a.log1p_alpha, a.variant, tid >> 4, 0)) << 16;
-    }
-    const int lane = tid & 63, w = tid >> 6;
-#pragma unroll
-    for (int r = 0; r < 16; ++r) {
-        const uint32_t x = __shfl(entry, 4 * r + (lane >> 4));
-        *reinterpret_cast<uint4 *>(lds + (size_t)(64 * w + 4 * r + (lane >> 4)) * 256 + 16 * (lane & 15)) =
-            make_uint4(x, x, x, x);
-    }
-    __syncthreads();
-}
-
 // Grid (worker, kv head x row chunk) for the contiguous layout, the kv head fastest
 // for paged ones (anchor_decode.hip); with a workgroup per unit the sequence in z.
 // WALK: the workgroup walks a list of segments.
 template <int MT, int FULL, int LAYOUT, bool WALK>
 __global__ __launch_bounds__(kThreads, 2) void hier_attn_kernel(HierArgs a) {
-    __shared__ __attribute__((aligned(1024))) uint8_t lds[kTable + kShare];
+    __shared__ __attribute__((aligned(1024))) uint8_t lds[kTableBytes + kShare];
     const int worker = LAYOUT == 0 ? blockIdx.x : blockIdx.y;
     const int hc = LAYOUT == 0 ? blockIdx.y : blockIdx.x;
     Segment<kWorkUnit> seg;
     if (!WALK) {
         if (!seg.set_unit(a.seq_lens, a.max_seq_len, a.direct, blockIdx.z, worker)) return;
-        if (seg.n_groups > 0) fill_table<FULL>(a, lds);
-        attend_segment<MT, FULL, LAYOUT>(a, seg, hc % a.geo.Hkv, hc / a.geo.Hkv, threadIdx.x, lds);
+        attend_segment<MT, FULL, LAYOUT, true>(a, seg, hc % a.geo.Hkv, hc / a.geo.Hkv, threadIdx.x, lds);
         return;
     }
     const WorkList<kWorkUnit, true> list(a.seq_lens, a.B, a.max_seq_len, a.workers);
     if (!seg.start(list, worker)) return;
     fill_table<FULL>(a, lds);
     for (;;) {
-        attend_segment<MT, FULL, LAYOUT>(a, seg, fresh_uniform(hc % a.geo.Hkv), fresh_uniform(hc / a.geo.Hkv), fresh_tid(), lds);
+        attend_segment<MT, FULL, LAYOUT, false>(a, seg, fresh_uniform(hc % a.geo.Hkv), fresh_uniform(hc / a.geo.Hkv),
+                                                fresh_tid(), lds);
         if (!seg.next(list, worker)) return;
         __syncthreads();  // the segment's LDS is free again
     }

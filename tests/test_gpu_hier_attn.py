@@ -125,6 +125,14 @@ def test_batches_of_many_units(B, most, bt, G, k, tail, full):
     Case(lens, 8, CENTRED if full else INT4, full, bt=bt, seed=B).check(8 * G, k, tail)
 
 
+@pytest.mark.parametrize("variant,full", FORMS)
+@pytest.mark.parametrize("lens,Hkv,G,k,tail,bt", [((31, 0, 700), 2, 4, 3, 5, 16), ((130, 97), 2, 8, 9, 9, 48),
+                                                  ((513,), 1, 5, 64, 64, 24), ((64, 1500), 1, 7, 20, 0, None)])
+def test_rows_of_many_tiles(variant, full, lens, Hkv, G, k, tail, bt):
+    """Fewer rows than a workgroup's, its number, and more."""
+    Case(lens, Hkv, variant, full, bt=bt, seed=sum(lens)).check(Hkv * G, k, tail)
+
+
 @pytest.mark.parametrize("alpha", [1e-38, 1e-5, 9e-5, 1.1e-4, 1.0, 15.0, 1e4, 1e30])
 def test_alpha(alpha):
     for variant, full in FORMS:
@@ -159,6 +167,8 @@ def test_zero_cache_and_constant_channels():
     z = torch.zeros(70, 1, 128, dtype=torch.bfloat16)
     Case([70], 1, INT4, kv=[(z, z)]).check(4)
     Case([70], 1, CENTRED, True, kv=[(z + 1.5, z - 2.0)]).check(4, 2, 2)
+    for k in (1, 9):  # queries of zeros too: every score is 0, what is masked is not
+        Case([70], 1, INT4, kv=[(z, z + 1.0)]).check(4, k, q=torch.zeros(1, k, 4, 128, dtype=torch.bfloat16))
 
 
 def test_bad_block_ids_poison_their_sequence_alone():
