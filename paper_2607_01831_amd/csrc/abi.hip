@@ -824,6 +824,18 @@ int lynx_qk_norm_rope(int32_t n_tokens, int32_t Hq, int32_t Hkv, int32_t head_di
     for (const void *p : may_be_null)
         if (!aligned16(p)) return LYNX_EINVAL;
     if (rotary_dim > 0 && !inv_freq) return LYNX_EINVAL;
+    // no output may overlap an input
+    const struct { const void *p; int64_t rows, stride, heads; } in[] = {
+        {q_bf16, n_tokens, q_stride, Hq}, {k_bf16, n_tokens, k_stride, Hkv}, {v_bf16, n_tokens, v_stride, Hkv}};
+    const struct { const void *p; int64_t heads; } out[] = {{q_out, Hq}, {k_out, Hkv}, {v_out, Hkv}};
+    for (const auto &i : in)
+        for (const auto &o : out) {
+            if (!i.p || !o.p) continue;
+            const uintptr_t i0 = reinterpret_cast<uintptr_t>(i.p), o0 = reinterpret_cast<uintptr_t>(o.p);
+            const uintptr_t i1 = i0 + ((i.rows - 1) * i.stride + i.heads * lynx::kHeadDim) * 2;
+            const uintptr_t o1 = o0 + (uintptr_t)n_rows * o.heads * lynx::kHeadDim * 2;
+            if (i0 < o1 && o0 < i1) return LYNX_EINVAL;
+        }
     lynx::RopeArgs a;
     a.n_tokens = n_tokens;
     a.Hq = Hq;

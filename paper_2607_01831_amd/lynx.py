@@ -954,6 +954,22 @@ class KVPool:
                        self.k_codes, self.v_codes, self.k_anc, self.v_anc, self.k_res, self.v_res, self.meta, stream)
 
 
+@dataclass
+class FreeBlocks:
+    """The blocks of a paged cache that no sequence has, and the sequences' table
+    (device): what lynx_blocks_extend and lynx_blocks_release keep."""
+    table: torch.Tensor  # int32 [B][max_blocks_per_seq], -1 where there is no block
+    stack: torch.Tensor  # int32 [num_blocks]
+    state: torch.Tensor  # int32 [2]: ids on the stack, 0
+
+    @staticmethod
+    def allocate(L: Layout, B: int, device="cuda") -> "FreeBlocks":
+        """Empty sequences, every block free, block 0 on top."""
+        i32 = dict(dtype=torch.int32, device=device)
+        return FreeBlocks(torch.full((B, L.max_blocks_per_seq), -1, **i32),
+                          torch.arange(L.num_blocks - 1, -1, -1, **i32), torch.tensor([L.num_blocks, 0], **i32))
+
+
 def contiguous_layout(Hkv: int, B: int, T: int) -> Layout:
     """One block of T tokens per sequence; block_table[b] = [b]."""
     return Layout(num_kv_heads=Hkv, block_tokens=T, max_blocks_per_seq=1, num_blocks=B,

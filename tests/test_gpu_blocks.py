@@ -107,7 +107,8 @@ class Pool:
 
 
 @pytest.mark.parametrize("bt", [1, 5, 16, 128])
-@pytest.mark.parametrize("B,most", [(1, 1), (1, 300), (3, 70), (64, 9), (255, 3), (256, 4), (257, 5), (1030, 2), (2100, 3)])
+@pytest.mark.parametrize("B,most", [(1, 1), (1, 300), (3, 70), (64, 9), (255, 3), (256, 4), (257, 5), (1030, 2), (2100, 3),
+                                    (20000, 2)])
 def test_extend_and_release(B, most, bt):
     r = np.random.default_rng(B * 131 + bt)
     lens = r.integers(0, 200, B).tolist()

@@ -26,9 +26,9 @@ def test_speculative_step(whole, monkeypatch):
     B, n_blocks = len(lens), 96
     L = lynx.Layout(num_kv_heads=H, block_tokens=bt, max_blocks_per_seq=per, num_blocks=n_blocks, max_tokens=per * bt)
     ints = lambda x: torch.tensor(x, dtype=torch.int32).cuda()  # noqa: E731
-    table = torch.full((B, per), -1, dtype=torch.int32).cuda()
-    stack = torch.randperm(n_blocks, generator=torch.Generator().manual_seed(1)).to(torch.int32).cuda()
-    state, zero = ints([n_blocks, 0]), ints([0] * B)
+    free = lynx.FreeBlocks.allocate(L, B)
+    table, stack, state, zero = free.table, free.stack, free.state, ints([0] * B)
+    stack.copy_(torch.randperm(n_blocks, generator=torch.Generator().manual_seed(1)))
     granted, starts = ints([0] * B), ints([0] * (B + 1))
     # the prompts' blocks, and their cache
     lynx.lynx_blocks_extend(L, B, 300, zero, ints(lens), table, stack, state, granted, starts)

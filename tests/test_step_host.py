@@ -52,8 +52,8 @@ def test_attn_hier_refusals(lib):
 
 
 def test_qk_norm_rope_refusals(lib):
-    def call(n=4, Hq=8, Hkv=2, D=128, q=16, qs=1536, k=16, ks=1536, v=16, vs=1536, pos=16, rows=None, n_rows=4, qw=16, kw=16,
-             eps=1e-6, freq=16, rotary=128, pairs=0, scale=1.0, qo=16, ko=16, vo=16):
+    def call(n=4, Hq=8, Hkv=2, D=128, q=1 << 20, qs=1536, k=1 << 20, ks=1536, v=1 << 20, vs=1536, pos=16, rows=None, n_rows=4,
+             qw=16, kw=16, eps=1e-6, freq=16, rotary=128, pairs=0, scale=1.0, qo=2 << 20, ko=3 << 20, vo=4 << 20):
         return lib.lynx_qk_norm_rope(n, Hq, Hkv, D, q, qs, k, ks, v, vs, pos, rows, n_rows, qw, kw, eps, freq, rotary, pairs,
                                      scale, qo, ko, vo, None)
     assert call(D=64) == E.LYNX_ENOTSUP
@@ -63,7 +63,8 @@ def test_qk_norm_rope_refusals(lib):
                 dict(rows=4), dict(n_rows=3), dict(n_rows=-1), dict(rows=16, n_rows=-1), dict(qw=8), dict(kw=8),
                 dict(eps=-1e-6), dict(eps=math.nan), dict(eps=math.inf), dict(freq=None), dict(freq=8), dict(rotary=-16),
                 dict(rotary=144), dict(rotary=24), dict(rotary=8), dict(pairs=2), dict(pairs=-1), dict(scale=math.nan),
-                dict(scale=math.inf), dict(qo=None), dict(qo=8), dict(ko=None), dict(ko=8)):
+                dict(scale=math.inf), dict(qo=None), dict(qo=8), dict(ko=None), dict(ko=8), dict(qo=1 << 20),
+                dict(ko=(1 << 20) + 3 * 3072 + 512 * 2 - 16), dict(vo=(1 << 20) - 4 * 256 * 2 + 16), dict(qo=(1 << 20) - 16)):
         assert call(**bad) == E.LYNX_EINVAL, bad
     none = dict(q=None, k=None, v=None, pos=None, qw=None, kw=None, freq=None, qo=None, ko=None, vo=None)
     assert call(n=0, **none) == E.LYNX_OK
