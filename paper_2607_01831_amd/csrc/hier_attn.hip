@@ -48,8 +48,8 @@ constexpr float kLog2e = 1.4426950408889634f;
 constexpr int kShare = 16384;
 
 // One segment of a worker's share, kv head h, rows r0 .. r0 + 16 MT - 1.
-// Wavefront w owns the 128-token groups w, w + 4, ... of the segment and attends
-// their chunks with an online softmax of its own: no barrier in the loop.
+// A wavefront owns a quarter of the segment's chunks and attends them with an online
+// softmax of its own: no barrier in the loop.
 //
 // Layouts of a wavefront's step (col = lane % 16, g = lane / 16): the scores are
 // computed as K Q^T, lane (col, g) holding query row col against tokens 4 g + i and
@@ -63,7 +63,6 @@ constexpr int kShare = 16384;
 template <int MT, int FULL, int LAYOUT, bool FILL>
 __device__ __forceinline__ void attend_segment(const HierArgs &a, const Segment<kWorkUnit> &seg, int h, int chunk_rows,
                                                const int tid, uint8_t *lds) {
-    static_assert(kWorkUnit == kWaves, "a group per wavefront and unit");
     constexpr int kRow = FULL ? kCodeRow : kNibbleRow;
     constexpr int kKW = FULL ? 8 : 4;  // words of a lane's K row quarter
     constexpr int kVW = FULL ? 2 : 1;  // words of a lane's 8 dims of a V row
@@ -104,12 +103,12 @@ __device__ __forceinline__ void attend_segment(const HierArgs &a, const Segment<
         return ((size_t)blk * Hkv + h) * a.geo.bt + (size_t)(t - block_index(t) * a.geo.bt);
     };
 
-    // ---- the wavefront's chunks ----
-    const int my_groups = seg.n_groups > w ? (seg.n_groups - w + kWaves - 1) / kWaves : 0;
-    auto chunk_t0 = [&](int j) { return (seg.g0 + w + kWaves * (j >> 2)) * kKGroup + kChunk * (j & 3); };
-    // the last group of the sequence may hold fewer than four
-    int n_mine = 4 * my_groups;
-    while (n_mine > 0 && chunk_t0(n_mine - 1) >= T) --n_mine;
+    // ---- the wavefront's chunks: a quarter of the segment's, one after the other ----
+    const int base_t = seg.g0 * kKGroup;
+    const int n_chunks = (min(seg.n_groups * kKGroup, T - base_t) + kChunk - 1) / kChunk;
+    const int c0 = __builtin_amdgcn_readfirstlane(n_chunks * w / kWaves);
+    const int n_mine = __builtin_amdgcn_readfirstlane(n_chunks * (w + 1) / kWaves) - c0;
+    auto chunk_t0 = [&](int j) { return base_t + kChunk * (c0 + j); };
 
     // ---- loads of a chunk: keys, values, scalars ----
     // Past the last chunk they load that one again: every step issues as many, so a
@@ -117,12 +116,11 @@ __device__ __forceinline__ void attend_segment(const HierArgs &a, const Segment<
     uint32_t rk[2][kKW];  // token 16 i + col, bytes kRow / 4 * g ..
     uint32_t rv[8][kVW];  // token slot e, dims 8 col .. + 7
     float2 rm[8];         // channels 2 lane, 2 lane + 1: K's sigma, mu, gscale, gmin, V's
-    // LAYOUT 1: the blocks of a group's eight 16-token runs, run r in lane r, loaded a
-    // group ahead of the rows (entries past the table's end are clamped and unused)
+    // LAYOUT 1: the blocks of four chunks' eight 16-token runs, run r in lane r, loaded
+    // four chunks ahead of the rows (entries past the table's end are clamped and unused)
     int ids = 0, ids_next = 0;
-    auto load_ids = [&](int u) {
-        if (LAYOUT == 1)
-            ids_next = bt_row[min(block_index((seg.g0 + w + kWaves * u) * kKGroup + 16 * (lane & 7)), a.geo.max_blocks - 1)];
+    auto load_ids = [&](int j) {
+        if (LAYOUT == 1) ids_next = bt_row[min(block_index(chunk_t0(j) + 16 * (lane & 7)), a.geo.max_blocks - 1)];
     };
     // The row's bytes of the tokens of chunk j that rows(i or e) asks for: run(i, row0)
     // for each of its two runs of 16 tokens where they lie in one block each, else
@@ -196,7 +194,7 @@ __device__ __forceinline__ void attend_segment(const HierArgs &a, const Segment<
     auto next_k = [&](int j) {
         if (LAYOUT == 1 && (j & 3) == 0 && j <= last) {
             ids = ids_next;
-            load_ids(min((j >> 2) + 1, my_groups - 1));
+            load_ids(j + 4);
         }
         load_k(min(j, last), ids);
     };
@@ -407,7 +405,6 @@ __device__ __forceinline__ void attend_segment(const HierArgs &a, const Segment<
         next_maps();
         load_meta(min(1, last));
         look_k(0);
-        if (kParts == 1) next_k(1);
     }
     for (int j = 0; j < n_mine; ++j) {
 #pragma unroll
@@ -420,7 +417,6 @@ __device__ __forceinline__ void attend_segment(const HierArgs &a, const Segment<
                 if (part + 2 == kParts) next_k(j + 1);
             } else {
                 look_v(0);
-                if (kParts == 1) load_v(min(j + 1, last), ids);
             }
             scores(part);
         }
@@ -434,7 +430,6 @@ __device__ __forceinline__ void attend_segment(const HierArgs &a, const Segment<
                 if (part + 2 == kParts) load_v(min(j + 1, last), ids);
             } else {
                 look_k(0);
-                if (kParts == 1) next_k(j + 2);
             }
             values(part);
         }
