@@ -7,13 +7,15 @@
 // dims turned by the angle position * inv_freq[i]; V is moved as it is.  fp32
 // throughout, rounded to BF16 once.
 //
-// It is bound by memory: every byte is read once and written once.  16 lanes hold a
-// head, 8 dims (16 bytes) each, so the mean is four DPP additions.  The angles are
-// a token's, not a head's: a workgroup computes the cosines and sines of its tokens
-// once, a pair a thread, and the lanes keep those of their 8 dims for all of a
-// token's heads.  The angle is taken in turns in double precision and reduced there
-// (a position of 2^31 turns by 1e-7 of a turn too much at most), its sine and
-// cosine in fp32.
+// It is bound by memory: every byte is read once and written once; a call of few
+// tokens by one launch's latency, 4.4 us with the host's.  16 lanes hold a head, 8
+// dims (16 bytes) each, so the mean is four DPP additions.  A workgroup takes 16 heads
+// of a token: 64 threads compute the token's cosines and sines while the heads' rows
+// are on their way.  2 and 4 tokens a workgroup read the same bytes with fewer angles
+// and were slower (2048 tokens of 32 + 8 + 8 heads 12.9 us, so 15.1 and 15.4; 16384
+// 79.4, so 78.0 and 79.3).
+// The angle is taken in turns in double precision and reduced there (a position of
+// 2^31 turns by 1e-7 of a turn too much at most), its sine and cosine in fp32.
 #include "lane_ops.h"
 #include "lynx_internal.h"
 
@@ -21,7 +23,8 @@ namespace lynx {
 namespace {
 
 constexpr int kThreads = 256;
-constexpr int kHeads = kThreads / 16;  // heads that a workgroup holds at once
+constexpr int kHeads = kThreads / 16;  // heads that a workgroup takes
+constexpr int kGridTokens = 65535;     // tokens along the grid's second axis
 
 __device__ __forceinline__ float bf16_lo(uint32_t w) { return __uint_as_float(w << 16); }
 __device__ __forceinline__ float bf16_hi(uint32_t w) { return __uint_as_float(w & 0xffff0000u); }
@@ -54,110 +57,89 @@ __device__ __forceinline__ uint4 partner(const uint4 &u, int from) {
     return make_uint4(__shfl(u.x, from), __shfl(u.y, from), __shfl(u.z, from), __shfl(u.w, from));
 }
 
-// Workgroup: TOKENS tokens, all their heads (gridDim.y 1) or every gridDim.y-th
-// group of 16.  The heads of a token: Q, K, V.
-template <Pairs PAIRS, int TOKENS>
+// Workgroup (heads / 16, tokens, tokens / 65535): 16 heads of a token, which has its Q,
+// K and V heads in that order.
+template <Pairs PAIRS>
 __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
     // by dim: cosine, and sine with the sign that its partner enters with
-    __shared__ __attribute__((aligned(16))) float s_cos[TOKENS][kHeadDim], s_sin[TOKENS][kHeadDim];
+    __shared__ __attribute__((aligned(16))) float s_cos[kHeadDim], s_sin[kHeadDim];
     const int tid = threadIdx.x, lane = tid & 63, c = tid & 15;
-    const int n0 = blockIdx.x * TOKENS;
+    const int64_t n = (int64_t)blockIdx.z * kGridTokens + blockIdx.y;
+    if (n >= a.n_tokens) return;
+    const int pos = a.positions[n];
+    const int64_t row = a.rows ? a.rows[n] : n;
     const int half = a.rotary / 2;
-    for (int i = tid; i < TOKENS * (kHeadDim / 2); i += kThreads) {
-        const int tok = i / (kHeadDim / 2), p = i % (kHeadDim / 2);
+    const int h = kHeads * (int)blockIdx.x + (tid >> 4);
+    const bool live = h < a.Hq + a.Hkv + (a.v ? a.Hkv : 0), is_q = h < a.Hq, is_v = h >= a.Hq + a.Hkv;
+    const int own = is_q ? h : is_v ? h - a.Hq - a.Hkv : h - a.Hq;
+    const int64_t stride = is_q ? a.q_stride : is_v ? a.v_stride : a.k_stride;
+    const uint16_t *src = (is_q ? a.q : is_v ? a.v : a.k) + (size_t)own * kHeadDim;
+    const uint4 u = live ? reinterpret_cast<const uint4 *>(src + n * stride)[c] : make_uint4(0u, 0u, 0u, 0u);
+    const uint16_t *weight = is_q ? a.q_weight : a.k_weight;
+    const uint4 wu = weight ? reinterpret_cast<const uint4 *>(weight)[c] : make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
+    if (tid < kHeadDim / 2) {
         float co = 1.0f, si = 0.0f;
-        int d0 = 2 * p, d1 = 2 * p + 1;  // the pair's dims; those past `rotary` stay as they are
-        if (p < half) {
-            const int pos = a.positions[min(n0 + tok, a.n_tokens - 1)];
-            double turns = (double)pos * ((double)a.inv_freq[p] * 0.15915494309189535);
+        int d0 = 2 * tid, d1 = 2 * tid + 1;  // the pair's dims; those past `rotary` stay as they are
+        if (tid < half) {
+            double turns = (double)pos * ((double)a.inv_freq[tid] * 0.15915494309189535);
             turns -= rint(turns);
             sincospif(2.0f * (float)turns, &si, &co);
             co *= a.scale;
             si *= a.scale;
             if (PAIRS != kNeighbours) {
-                d0 = p;
-                d1 = p + half;
+                d0 = tid;
+                d1 = tid + half;
             }
         }
-        s_cos[tok][d0] = co;
-        s_cos[tok][d1] = co;
-        s_sin[tok][d0] = -si;
-        s_sin[tok][d1] = si;
+        s_cos[d0] = co;
+        s_cos[d1] = co;
+        s_sin[d0] = -si;
+        s_sin[d1] = si;
     }
     // the lane that holds the partners of this lane's dims
     int from = lane;
     if (PAIRS == kHalves && 8 * c < a.rotary) from = 8 * c < half ? lane + half / 8 : lane - half / 8;
-    float wq[8], wk[8], pq[8], pk[8];  // weights of the lane's dims and of their partners
-    {
-        const uint4 one = make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
-        const uint4 q = a.q_weight ? reinterpret_cast<const uint4 *>(a.q_weight)[c] : one;
-        const uint4 k = a.k_weight ? reinterpret_cast<const uint4 *>(a.k_weight)[c] : one;
-        unpack8(q, wq);
-        unpack8(k, wk);
-        unpack8(partner<PAIRS>(q, from), pq);
-        unpack8(partner<PAIRS>(k, from), pk);
-    }
+    float w[8], pw[8];  // weights of the lane's dims and of their partners
+    unpack8(wu, w);
+    unpack8(partner<PAIRS>(wu, from), pw);
     __syncthreads();
-    const int heads = a.Hq + a.Hkv + (a.v ? a.Hkv : 0);
-#pragma unroll 1
-    for (int tok = 0; tok < TOKENS; ++tok) {
-        const int n = n0 + tok;
-        if (n >= a.n_tokens) break;
-        const int pos = a.positions[n];
-        const int64_t row = a.rows ? a.rows[n] : n;
-        if (pos < 0 || row < 0 || row >= a.n_rows) continue;
-        float co[8], si[8];
+    if (pos < 0 || row < 0 || row >= a.n_rows) return;  // (here, so that no load waits for it)
+    float x[8], p[8];
+    unpack8(u, x);
+    unpack8(partner<PAIRS>(u, from), p);
+    float ss = 0.0f;
 #pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const float4 x = reinterpret_cast<const float4 *>(s_cos[tok])[2 * c + i];
-            const float4 y = reinterpret_cast<const float4 *>(s_sin[tok])[2 * c + i];
-            co[4 * i] = x.x; co[4 * i + 1] = x.y; co[4 * i + 2] = x.z; co[4 * i + 3] = x.w;
-            si[4 * i] = y.x; si[4 * i + 1] = y.y; si[4 * i + 2] = y.z; si[4 * i + 3] = y.w;
+    for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
+    ss = row16_sum(ss);
+    const float r = weight ? 1.0f / sqrtf(ss * (1.0f / kHeadDim) + a.eps) : 1.0f;
+    uint32_t o[4];
+#pragma unroll
+    for (int i = 0; i < 8; i += 4) {
+        const float4 co4 = reinterpret_cast<const float4 *>(s_cos)[2 * c + i / 4];
+        const float4 si4 = reinterpret_cast<const float4 *>(s_sin)[2 * c + i / 4];
+        const float co[4] = {co4.x, co4.y, co4.z, co4.w}, si[4] = {si4.x, si4.y, si4.z, si4.w};
+        float y[4];
+#pragma unroll
+        for (int k = 0; k < 4; ++k) {
+            const float xw = x[i + k] * r * w[i + k], yw = p[i + k] * r * pw[i + k];
+            // (a dim past `rotary` is its own partner's no one: cosine 1, no product with an infinity)
+            y[k] = 8 * c < a.rotary ? fmaf(yw, si[k], xw * co[k]) : xw;
         }
-        for (int h0 = kHeads * blockIdx.y; h0 < heads; h0 += kHeads * gridDim.y) {
-            const int h = h0 + (tid >> 4);
-            const bool is_q = h < a.Hq, is_v = h >= a.Hq + a.Hkv;
-            const int own = is_q ? h : is_v ? h - a.Hq - a.Hkv : h - a.Hq;
-            const uint16_t *src = is_q ? a.q + (size_t)n * a.q_stride : is_v ? a.v + (size_t)n * a.v_stride : a.k + (size_t)n * a.k_stride;
-            uint16_t *dst = is_q ? a.q_out + (size_t)row * a.Hq * kHeadDim : (is_v ? a.v_out : a.k_out) + (size_t)row * a.Hkv * kHeadDim;
-            const bool live = h < heads;
-            const uint4 u = live ? reinterpret_cast<const uint4 *>(src + (size_t)own * kHeadDim)[c] : make_uint4(0u, 0u, 0u, 0u);
-            const uint4 pu = partner<PAIRS>(u, from);
-            float x[8], p[8];
-            unpack8(u, x);
-            unpack8(pu, p);
-            float ss = 0.0f;
-#pragma unroll
-            for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
-            ss = row16_sum(ss);
-            const bool normed = is_q ? a.q_weight != nullptr : a.k_weight != nullptr;
-            const float r = normed ? 1.0f / sqrtf(ss * (1.0f / kHeadDim) + a.eps) : 1.0f;
-            uint32_t o[4];
-#pragma unroll
-            for (int i = 0; i < 8; i += 2) {
-                float y[2];
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const float xw = x[i + k] * r * (is_q ? wq[i + k] : wk[i + k]);
-                    const float pw = p[i + k] * r * (is_q ? pq[i + k] : pk[i + k]);
-                    // (a dim past `rotary` is its own partner's no one: cosine 1, no product with an infinity)
-                    y[k] = 8 * c < a.rotary ? fmaf(pw, si[i + k], xw * co[i + k]) : xw;
-                }
-                o[i / 2] = pack2(y[0], y[1]);
-            }
-            if (live)
-                reinterpret_cast<uint4 *>(dst + (size_t)own * kHeadDim)[c] = is_v ? u : make_uint4(o[0], o[1], o[2], o[3]);
-        }
+        o[i / 2] = pack2(y[0], y[1]);
+        o[i / 2 + 1] = pack2(y[2], y[3]);
+    }
+    if (live) {
+        uint16_t *dst = is_q ? a.q_out + (size_t)row * a.Hq * kHeadDim : (is_v ? a.v_out : a.k_out) + (size_t)row * a.Hkv * kHeadDim;
+        reinterpret_cast<uint4 *>(dst + (size_t)own * kHeadDim)[c] = is_v ? u : make_uint4(o[0], o[1], o[2], o[3]);
     }
 }
 
 template <Pairs PAIRS>
 void launch_pairs(const RopeArgs &a, hipStream_t stream) {
-    const int heads = a.Hq + a.Hkv + (a.v ? a.Hkv : 0), groups = (heads + kHeads - 1) / kHeads;
-    if (a.n_tokens >= 2048)
-        hipLaunchKernelGGL((rope_kernel<PAIRS, 4>), dim3((a.n_tokens + 3) / 4), dim3(kThreads), 0, stream, a);
-    else
-        hipLaunchKernelGGL((rope_kernel<PAIRS, 1>), dim3(a.n_tokens, groups), dim3(kThreads), 0, stream, a);
+    const int heads = a.Hq + a.Hkv + (a.v ? a.Hkv : 0);
+    const dim3 grid((heads + kHeads - 1) / kHeads, a.n_tokens < kGridTokens ? a.n_tokens : kGridTokens,
+                    (unsigned)(((int64_t)a.n_tokens + kGridTokens - 1) / kGridTokens));
+    hipLaunchKernelGGL((rope_kernel<PAIRS>), grid, dim3(kThreads), 0, stream, a);
 }
 
 }  // namespace

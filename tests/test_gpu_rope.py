@@ -78,6 +78,11 @@ def test_tokens_and_heads(tokens, Hq, Hkv):
     check(tokens, Hq, Hkv, 128, tokens % 2 == 1, fused=tokens % 3 != 0)
 
 
+def test_more_tokens_than_a_grid_axis():
+    for tokens in (65535, 65536, 131077):
+        check(tokens, 1, 1, 16, False, seed=5)
+
+
 @pytest.mark.parametrize("norm", [(False, False), (True, False), (False, True)])
 def test_without_norms(norm):
     for tokens in (7, 2100):
