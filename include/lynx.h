@@ -770,8 +770,8 @@ int lynx_attn_hier(const lynx_layout *L, int32_t B, int32_t Hq, int32_t k, int32
  *   scale        of the rotated dims (1, or a long-context factor)
  *   q_out        BF16 [n_rows][Hq][128]; k_out, v_out BF16 [n_rows][Hkv][128]
  *                (device, written; rows of no token are left as they were).
- *                None may overlap an input (LYNX_EINVAL: the bytes between an
- *                input's first token and the end of its last count)
+ *                None may overlap an input or another (LYNX_EINVAL: the bytes
+ *                between an input's first token and the end of its last count)
  */
 int lynx_qk_norm_rope(int32_t n_tokens, int32_t Hq, int32_t Hkv, int32_t head_dim,
                       const void *q_bf16, int64_t q_stride, const void *k_bf16, int64_t k_stride,
@@ -817,7 +817,7 @@ int lynx_qk_norm_rope(int32_t n_tokens, int32_t Hq, int32_t Hkv, int32_t head_di
  *                outside [0, num_blocks); and its row b * n_src + i in arrays
  *                [B][n_src] (new token i of the sequence), as `rows` of
  *                lynx_qk_norm_rope fills them.  -1 from starts[B] on
- * granted and starts must not be counts or seq_lens; num_blocks * block_tokens and
+ * No written array may overlap another (LYNX_EINVAL); num_blocks * block_tokens and
  * B * max_blocks_per_seq must be less than 2^31.  B <= 65535.  Launches one kernel.
  */
 int lynx_blocks_extend(const lynx_layout *L, int32_t B, int32_t n_src, int32_t max_rows,

@@ -824,13 +824,14 @@ int lynx_qk_norm_rope(int32_t n_tokens, int32_t Hq, int32_t Hkv, int32_t head_di
     for (const void *p : may_be_null)
         if (!aligned16(p)) return LYNX_EINVAL;
     if (rotary_dim > 0 && !inv_freq) return LYNX_EINVAL;
-    // no output may overlap an input
+    // no output may overlap an input or another output
     const struct { const void *p; int64_t rows, stride, heads; } in[] = {
-        {q_bf16, n_tokens, q_stride, Hq}, {k_bf16, n_tokens, k_stride, Hkv}, {v_bf16, n_tokens, v_stride, Hkv}};
+        {q_bf16, n_tokens, q_stride, Hq}, {k_bf16, n_tokens, k_stride, Hkv}, {v_bf16, n_tokens, v_stride, Hkv},
+        {q_out, n_rows, (int64_t)Hq * lynx::kHeadDim, Hq}, {k_out, n_rows, (int64_t)Hkv * lynx::kHeadDim, Hkv}};
     const struct { const void *p; int64_t heads; } out[] = {{q_out, Hq}, {k_out, Hkv}, {v_out, Hkv}};
     for (const auto &i : in)
         for (const auto &o : out) {
-            if (!i.p || !o.p) continue;
+            if (!i.p || !o.p || &i - in == &o - out + 3) continue;
             const uintptr_t i0 = reinterpret_cast<uintptr_t>(i.p), o0 = reinterpret_cast<uintptr_t>(o.p);
             const uintptr_t i1 = i0 + ((i.rows - 1) * i.stride + i.heads * lynx::kHeadDim) * 2;
             const uintptr_t o1 = o0 + (uintptr_t)n_rows * o.heads * lynx::kHeadDim * 2;
@@ -890,6 +891,23 @@ int blocks_args(const lynx_layout *L, int32_t B, const int32_t *seq_lens, const 
     a->state = free_state;
     return LYNX_OK;
 }
+
+// Whether an array that a call writes overlaps another of its arrays (the first
+// `read` of them are only read): every workgroup reads what others read too.
+struct Words {
+    const int32_t *p;
+    long long n;
+};
+template <int N>
+bool overlap(const Words (&w)[N], int read) {
+    for (int i = read; i < N; ++i)
+        for (int j = 0; j < i; ++j) {
+            if (!w[i].p || !w[j].p) continue;
+            const uintptr_t a0 = reinterpret_cast<uintptr_t>(w[i].p), b0 = reinterpret_cast<uintptr_t>(w[j].p);
+            if (a0 < b0 + 4ull * w[j].n && b0 < a0 + 4ull * w[i].n) return true;
+        }
+    return false;
+}
 }  // namespace
 
 extern "C" {
@@ -909,8 +927,10 @@ int lynx_blocks_extend(const lynx_layout *L, int32_t B, int32_t n_src, int32_t m
     const void *may_be_null[] = {seq_of, positions, slots, rows};
     for (const void *p : may_be_null)
         if (!aligned16(p)) return LYNX_EINVAL;
-    // what every workgroup reads is written by none
-    if (granted == counts || granted == seq_lens || starts == counts || starts == seq_lens) return LYNX_EINVAL;
+    const Words words[] = {{seq_lens, B}, {counts, B}, {free_blocks, a.num_blocks},
+                           {block_table, (long long)B * a.max_blocks}, {free_state, 2}, {granted, B}, {starts, B + 1},
+                           {seq_of, max_rows}, {positions, max_rows}, {slots, max_rows}, {rows, max_rows}};
+    if (overlap(words, 3)) return LYNX_EINVAL;
     a.n_src = n_src;
     a.max_rows = max_rows;
     a.granted = granted;
@@ -929,6 +949,9 @@ int lynx_blocks_release(const lynx_layout *L, int32_t B, const int32_t *seq_lens
     int rc = blocks_args(L, B, seq_lens, keep, block_table, free_blocks, free_state, &a);
     if (rc != LYNX_OK) return rc;
     if (B == 0) return LYNX_OK;
+    const Words words[] = {{seq_lens, B}, {keep, B}, {free_blocks, a.num_blocks},
+                           {block_table, (long long)B * a.max_blocks}, {free_state, 2}};
+    if (overlap(words, 2)) return LYNX_EINVAL;
     hipError_t e = lynx::launch_blocks_release(a, static_cast<hipStream_t>(stream));
     return e == hipSuccess ? LYNX_OK : LYNX_EHIP;
 }

@@ -64,29 +64,41 @@ def test_qk_norm_rope_refusals(lib):
                 dict(eps=-1e-6), dict(eps=math.nan), dict(eps=math.inf), dict(freq=None), dict(freq=8), dict(rotary=-16),
                 dict(rotary=144), dict(rotary=24), dict(rotary=8), dict(pairs=2), dict(pairs=-1), dict(scale=math.nan),
                 dict(scale=math.inf), dict(qo=None), dict(qo=8), dict(ko=None), dict(ko=8), dict(qo=1 << 20),
-                dict(ko=(1 << 20) + 3 * 3072 + 512 * 2 - 16), dict(vo=(1 << 20) - 4 * 256 * 2 + 16), dict(qo=(1 << 20) - 16)):
+                dict(ko=(1 << 20) + 3 * 3072 + 512 * 2 - 16), dict(vo=(1 << 20) - 4 * 256 * 2 + 16), dict(qo=(1 << 20) - 16),
+                dict(ko=2 << 20), dict(vo=3 << 20), dict(vo=(2 << 20) + 4 * 8 * 256 - 16)):
         assert call(**bad) == E.LYNX_EINVAL, bad
     none = dict(q=None, k=None, v=None, pos=None, qw=None, kw=None, freq=None, qo=None, ko=None, vo=None)
     assert call(n=0, **none) == E.LYNX_OK
 
 
 def test_blocks_refusals(lib):
-    def extend(L=None, B=2, n_src=4, rows=8, ins=(16,) * 5, outs=(112, 128), arrays=(16,) * 4):
+    K = 1 << 20  # (what lies where: no two arrays overlap)
+    INS, OUTS, ARRAYS = tuple(K * i for i in range(1, 6)), (6 * K, 7 * K), tuple(K * i for i in range(8, 12))
+
+    def extend(L=None, B=2, n_src=4, rows=8, ins=INS, outs=OUTS, arrays=ARRAYS):
         return lib.lynx_blocks_extend(ctypes.byref((L or _layout()).c()), B, n_src, rows, *ins, *outs, *arrays, None)
 
-    def release(L=None, B=2, ins=(16,) * 5):
+    def release(L=None, B=2, ins=INS):
         return lib.lynx_blocks_release(ctypes.byref((L or _layout()).c()), B, *ins, None)
+
+    def but(t, i, p):
+        return tuple(p if j == i else x for j, x in enumerate(t))
     for call in (extend, release):
         for bad in (dict(B=-1), dict(B=65536), dict(L=_layout(block_tokens=0)), dict(L=_layout(num_blocks=1 << 27)),
                     dict(L=_layout(max_blocks_per_seq=1 << 30)),
-                    *(dict(ins=tuple(p if j == i else 16 for j in range(5))) for i in range(5) for p in (None, 24))):
+                    *(dict(ins=but(INS, i, p)) for i in range(5) for p in (None, K * (i + 1) + 8)),
+                    # (lengths, counts, table, stack, its counter)
+                    dict(ins=but(INS, 2, INS[0])), dict(ins=but(INS, 2, INS[1] - 16)), dict(ins=but(INS, 4, INS[0])),
+                    dict(ins=but(INS, 4, INS[3])), dict(ins=but(INS, 2, INS[3]))):
             assert call(**bad) == E.LYNX_EINVAL, bad
         assert call(L=_layout(head_dim=64)) == E.LYNX_ENOTSUP
         assert call(B=0, ins=(None,) * 5) == E.LYNX_OK
-    for bad in (dict(n_src=-1), dict(n_src=1 << 30), dict(rows=-1), dict(rows=(1 << 30) + 1), dict(outs=(None, 128)),
-                dict(outs=(112, None)), dict(outs=(120, 128)), dict(arrays=(8, 16, 16, 16)), dict(arrays=(16, 16, 16, 8)),
-                dict(ins=(16, 112, 16, 16, 16)), dict(ins=(128, 16, 16, 16, 16)), dict(ins=(112, 16, 16, 16, 16)),
-                dict(ins=(16, 128, 16, 16, 16))):
+    for bad in (dict(n_src=-1), dict(n_src=1 << 30), dict(rows=-1), dict(rows=(1 << 30) + 1), dict(outs=but(OUTS, 0, None)),
+                dict(outs=but(OUTS, 1, None)), dict(outs=but(OUTS, 0, 6 * K + 8)), dict(arrays=but(ARRAYS, 0, 8)),
+                dict(arrays=but(ARRAYS, 3, 8)), dict(outs=but(OUTS, 0, INS[1])), dict(outs=but(OUTS, 1, INS[0])),
+                dict(outs=but(OUTS, 1, INS[1])), dict(outs=but(OUTS, 0, OUTS[1])), dict(arrays=but(ARRAYS, 1, INS[0])),
+                dict(arrays=but(ARRAYS, 2, INS[0] - 16)), dict(arrays=but(ARRAYS, 3, INS[2])),
+                dict(arrays=but(ARRAYS, 0, ARRAYS[1] + 16)), dict(arrays=but(ARRAYS, 1, INS[4]))):
         assert extend(**bad) == E.LYNX_EINVAL, bad
 
 
