@@ -24,6 +24,23 @@
 // operands in fp16's range whatever the cache's: K and V are scaled by an exponent
 // each that brings the largest |b| + |m| so far below 2^14, so values 2^-28 of the
 // largest lose bits; a query row by its largest element.
+//
+// What bounds it.  Long decodes, memory: 4 sequences of 64K, 64 heads over 8, 84.5 us,
+// 419 MB, 5.0 TB/s (a large copy 5.1); with its loads left out the same takes 58 us.
+// Many rows, the vector ALU and LDS: per 32 tokens a wavefront makes operands in
+// some 250 vector instructions (a v_perm, a packed multiply-add or a conversion takes
+// 4.5 cycles of its SIMD) and 64 lookups (2.3 cycles of the CU's LDS each, 128 from
+// merged codes), then 35 instructions and 16 matrix products per 16 rows; 20 queries
+// over 32K of merged codes, 80 rows a kv head, 60.5 us.  Short ones, the launch and a
+// chain of latencies: 4K 13.2 us.
+// Why so: the levels by table, since the transform's inverse is an exponential per
+// element; 64 copies of it, so that an address is one instruction (32 copies are read
+// as fast, but take two); lookups in batches of 16, what LDS counts; queries of 32 rows
+// at most, what two wavefronts a SIMD hold (64 and 80 rows at one a SIMD: 71 and 99 us
+// for the 60.5).  Operands made once for 64 to 256 rows by 8 wavefronts through LDS
+// cost more up to 64 rows a kv head (38 us, so 40; 32K) and gain from 128 on (70 us,
+// so 59; 512 rows of 2 x 16K 157 us, so 120), with four times the partials that
+// lynx_attn_workspace_bytes has room for; with those that it has they lose.
 #include "f16_ops.h"
 #include "hier_ops.h"
 #include "lane_ops.h"
@@ -122,9 +139,8 @@ __device__ __forceinline__ void attend_segment(const HierArgs &a, const Segment<
     auto load_ids = [&](int j) {
         if (LAYOUT == 1) ids_next = bt_row[min(block_index(chunk_t0(j) + 16 * (lane & 7)), a.geo.max_blocks - 1)];
     };
-    // The row's bytes of the tokens of chunk j that rows(i or e) asks for: run(i, row0)
-    // for each of its two runs of 16 tokens where they lie in one block each, else
-    // each(row_of), row_of(t) the row of token t of the chunk
+    // Where chunk j's rows are: run(i, offset of the first) for its two runs of 16 tokens
+    // where each lies in one block, else each(row_of), row_of(t) the offset of its token t.
     auto rows_of_chunk = [&](int j, int run_ids, auto run, auto each) {
         const int t0 = __builtin_amdgcn_readfirstlane(chunk_t0(j));
         if (LAYOUT != 2 && t0 + kChunk <= T) {
@@ -571,6 +587,10 @@ void launch_layout(const HierArgs &args, dim3 grid, hipStream_t stream) {
 
 }  // namespace
 
+// 32 rows a workgroup where there are more than 16, whose operands are then made half
+// as often: 20 rows of 32K 26.7 us, so 29.9 in tiles of 16; 80 rows 61.5, so 71.2;
+// 16 paged sequences of 1K-8K with 20 rows 55, so 70 (32 rows of 2000 tokens, all
+// latency, 20.3, so 17.4).
 hipError_t launch_hier_attn(const HierArgs &args, hipStream_t stream) {
     if (args.workers < 1 || args.workers > 65535) return hipErrorInvalidValue;
     const int tile = args.rows_total > 16 ? 32 : 16;

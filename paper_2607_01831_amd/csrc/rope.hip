@@ -7,13 +7,15 @@
 // dims turned by the angle position * inv_freq[i]; V is moved as it is.  fp32
 // throughout, rounded to BF16 once.
 //
-// It is bound by memory: every byte is read once and written once; a call of few
-// tokens by one launch's latency, 4.4 us with the host's.  16 lanes hold a head, 8
-// dims (16 bytes) each, so the mean is four DPP additions.  A workgroup takes 16 heads
-// of a token: 64 threads compute the token's cosines and sines while the heads' rows
-// are on their way.  2 and 4 tokens a workgroup read the same bytes with fewer angles
-// and were slower (2048 tokens of 32 + 8 + 8 heads 12.9 us, so 15.1 and 15.4; 16384
-// 79.4, so 78.0 and 79.3).
+// It is bound by memory: every byte is read once and written once (16384 tokens of
+// 32 + 8 + 8 heads 73.7 us, 403 MB, 5.5 TB/s; a large copy 5.1); a call of few tokens
+// by one launch's latency, 4.0 us with the host's.  16 lanes hold a head, 8 dims (16
+// bytes) each, so the mean is four DPP additions, and a pair's other half comes from
+// its lane by one more, normed.  A workgroup takes 16 heads of a token: 64 threads
+// compute the token's cosines and sines while the heads' rows are on their way.
+// Tokens two and four to a workgroup need fewer angles and were slower: before pairs
+// were exchanged normed (each lane then made its partners' too), 2048 tokens took 12.9
+// us, so 15.1 and 15.4; 16384 79.4, so 78.0 and 79.3; now 12.6 and 75.3.
 // The angle is taken in turns in double precision and reduced there (a position of
 // 2^31 turns by 1e-7 of a turn too much at most), its sine and cosine in fp32.
 #include "lane_ops.h"
@@ -46,16 +48,16 @@ __device__ __forceinline__ void unpack8(const uint4 &u, float *x) {
 // dims), or rotary / 2 dims away, a whole number of lanes: 8 of 16, or any.
 enum Pairs { kNeighbours, kHalves64, kHalves };
 
-__device__ __forceinline__ uint32_t swap_halves(uint32_t v) {  // with lane ^ 8 of the row of 16
-    return (uint32_t)__builtin_amdgcn_mov_dpp((int)v, 0x128, 0xF, 0xF, false);  // row_ror:8
-}
 template <Pairs PAIRS>
-__device__ __forceinline__ uint4 partner(const uint4 &u, int from) {
-    if (PAIRS == kNeighbours)
-        return make_uint4(u.x << 16 | u.x >> 16, u.y << 16 | u.y >> 16, u.z << 16 | u.z >> 16, u.w << 16 | u.w >> 16);
-    if (PAIRS == kHalves64) return make_uint4(swap_halves(u.x), swap_halves(u.y), swap_halves(u.z), swap_halves(u.w));
-    return make_uint4(__shfl(u.x, from), __shfl(u.y, from), __shfl(u.z, from), __shfl(u.w, from));
+__device__ __forceinline__ float partner(const float *x, int i, int from) {
+    if (PAIRS == kNeighbours) return x[i ^ 1];
+    if (PAIRS == kHalves64)  // lane ^ 8 of the row of 16: row_ror:8
+        return __int_as_float(__builtin_amdgcn_mov_dpp(__float_as_int(x[i]), 0x128, 0xF, 0xF, false));
+    return __shfl(x[i], from);
 }
+// Where dim d's cosine and sine are: so that the 16 lanes of a head read 256 bytes in a
+// row, twice.
+__device__ __forceinline__ int place(int d) { return ((d & 4) << 4) | ((d >> 3) << 2) | (d & 3); }
 
 // Workgroup (heads / 16, tokens, tokens / 65535): 16 heads of a token, which has its Q,
 // K and V heads in that order.
@@ -76,7 +78,7 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
     const uint16_t *src = (is_q ? a.q : is_v ? a.v : a.k) + (size_t)own * kHeadDim;
     const uint4 u = live ? reinterpret_cast<const uint4 *>(src + n * stride)[c] : make_uint4(0u, 0u, 0u, 0u);
     const uint16_t *weight = is_q ? a.q_weight : a.k_weight;
-    const uint4 wu = weight ? reinterpret_cast<const uint4 *>(weight)[c] : make_uint4(0x3f803f80u, 0x3f803f80u, 0x3f803f80u, 0x3f803f80u);
+    const uint4 wu = weight ? reinterpret_cast<const uint4 *>(weight)[c] : make_uint4(0u, 0u, 0u, 0u);
     if (tid < kHeadDim / 2) {
         float co = 1.0f, si = 0.0f;
         int d0 = 2 * tid, d1 = 2 * tid + 1;  // the pair's dims; those past `rotary` stay as they are
@@ -91,39 +93,39 @@ __global__ __launch_bounds__(kThreads) void rope_kernel(RopeArgs a) {
                 d1 = tid + half;
             }
         }
-        s_cos[d0] = co;
-        s_cos[d1] = co;
-        s_sin[d0] = -si;
-        s_sin[d1] = si;
+        s_cos[place(d0)] = co;
+        s_cos[place(d1)] = co;
+        s_sin[place(d0)] = -si;
+        s_sin[place(d1)] = si;
     }
     // the lane that holds the partners of this lane's dims
     int from = lane;
     if (PAIRS == kHalves && 8 * c < a.rotary) from = 8 * c < half ? lane + half / 8 : lane - half / 8;
-    float w[8], pw[8];  // weights of the lane's dims and of their partners
-    unpack8(wu, w);
-    unpack8(partner<PAIRS>(wu, from), pw);
     __syncthreads();
     if (pos < 0 || row < 0 || row >= a.n_rows) return;  // (here, so that no load waits for it)
-    float x[8], p[8];
+    float x[8], w[8];
     unpack8(u, x);
-    unpack8(partner<PAIRS>(u, from), p);
-    float ss = 0.0f;
+    if (weight) {
+        unpack8(wu, w);
+        float ss = 0.0f;
 #pragma unroll
-    for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
-    ss = row16_sum(ss);
-    const float r = weight ? 1.0f / sqrtf(ss * (1.0f / kHeadDim) + a.eps) : 1.0f;
+        for (int i = 0; i < 8; ++i) ss = fmaf(x[i], x[i], ss);
+        const float r = rsqrtf(row16_sum(ss) * (1.0f / kHeadDim) + a.eps);
+#pragma unroll
+        for (int i = 0; i < 8; ++i) x[i] = x[i] * r * w[i];
+    }
     uint32_t o[4];
 #pragma unroll
     for (int i = 0; i < 8; i += 4) {
-        const float4 co4 = reinterpret_cast<const float4 *>(s_cos)[2 * c + i / 4];
-        const float4 si4 = reinterpret_cast<const float4 *>(s_sin)[2 * c + i / 4];
+        const float4 co4 = reinterpret_cast<const float4 *>(s_cos)[4 * i + c];
+        const float4 si4 = reinterpret_cast<const float4 *>(s_sin)[4 * i + c];
         const float co[4] = {co4.x, co4.y, co4.z, co4.w}, si[4] = {si4.x, si4.y, si4.z, si4.w};
         float y[4];
 #pragma unroll
         for (int k = 0; k < 4; ++k) {
-            const float xw = x[i + k] * r * w[i + k], yw = p[i + k] * r * pw[i + k];
-            // (a dim past `rotary` is its own partner's no one: cosine 1, no product with an infinity)
-            y[k] = 8 * c < a.rotary ? fmaf(yw, si[k], xw * co[k]) : xw;
+            y[k] = fmaf(partner<PAIRS>(x, i + k, from), si[k], x[i + k] * co[k]);
+            // (a dim past `rotary` has no partner: no product of 0 with an infinity)
+            if (PAIRS != kHalves64 && 8 * c >= a.rotary) y[k] = x[i + k];
         }
         o[i / 2] = pack2(y[0], y[1]);
         o[i / 2 + 1] = pack2(y[2], y[3]);
