@@ -28,7 +28,7 @@
 // What bounds it.  Long decodes, memory: 4 sequences of 64K, 64 heads over 8, 84.5 us,
 // 419 MB, 5.0 TB/s (a large copy 5.1); with its loads left out the same takes 58 us.
 // Many rows, the vector ALU and LDS: per 32 tokens a wavefront makes operands in
-// some 250 vector instructions (a v_perm, a packed multiply-add or a conversion takes
+// some 250 vector instructions (450 from merged codes; a v_perm, a packed multiply-add or a conversion takes
 // 4.5 cycles of its SIMD) and 64 lookups (2.3 cycles of the CU's LDS each, 128 from
 // merged codes), then 35 instructions and 16 matrix products per 16 rows; 20 queries
 // over 32K of merged codes, 80 rows a kv head, 60.5 us.  Short ones, the launch and a
