@@ -28,6 +28,7 @@ struct AttnArgs {
     int tail;             // attend the BF16 tail
     int tail_first;       // tokens of the tail that query 0 sees; query i sees i more
     int tail_stride;      // tail tokens stored per sequence in k_new / v_new
+    bool even = false;    // the partials are those of start_even (work_list.h)
     const int32_t *seq_lens;
     const uint16_t *q;
     const uint16_t *k_new;
@@ -59,8 +60,8 @@ constexpr int kCombineThreads = 256;
 // kernel needs first (the first kBatch splits' partials, the tail's values,
 // and the query and tail keys for the tail scores) is issued before any of
 // them is used, so the kernel waits for memory once for up to 8 kBatch
-// splits.
-template <int kBatch>
+// splits.  EVEN: AttnArgs::even.
+template <int kBatch, bool EVEN>
 __global__ __launch_bounds__(kCombineThreads) void attn_combine_kernel(AttnArgs a, uint16_t *out,
                                                                        float *lse) {
     const int gr = blockIdx.x;
@@ -101,7 +102,7 @@ __global__ __launch_bounds__(kCombineThreads) void attn_combine_kernel(AttnArgs 
     using List = WorkList<kWorkUnit, false>;
     int n = a.max_live, seg0 = b * a.direct;
     const bool listed = !a.direct && a.B > 1;
-    if (listed) List(a.seq_lens, a.B, a.max_seq_len, a.workers).partials(b, seg0, n);
+    if (listed) List(a.seq_lens, a.B, a.max_seq_len, a.workers).template partials<EVEN>(b, seg0, n);
     const size_t base = ((size_t)h * a.rows_total + gr) * a.n_seg + seg0;
     // a batch of partials: splits s0, s0 + 8, ... (clamped to the last split)
     float4 v[kBatch];
@@ -242,10 +243,10 @@ __global__ __launch_bounds__(kCombineThreads) void attn_combine_kernel(AttnArgs 
 // paged sequences: 17.1 -> 8.1 us).
 // FIND: how the row's partials are found: 0 without the list, 1 by the list of a
 // batch whose sequences have a lane each, 2 by any list (32 sequences of 1K-8K:
-// 5.5 us, 5.7 by one kernel for all three).
+// 5.5 us, 5.7 by one kernel for all three), 3 as 1 where AttnArgs::even.
 template <int ROWS, int FIND>
 __global__ __launch_bounds__(32 * ROWS) void attn_combine_rows_kernel(AttnArgs a, uint16_t *out, float *lse) {
-    if (FIND == 1) __builtin_assume(a.B > 1 && a.B <= 64);
+    if (FIND == 1 || FIND == 3) __builtin_assume(a.B > 1 && a.B <= 64);
     constexpr int kThreads = 32 * ROWS;
     constexpr int kTailMax = 64;
     constexpr int kTokens = kThreads / 4;  // tail tokens scored per pass, four threads each
@@ -302,7 +303,7 @@ __global__ __launch_bounds__(32 * ROWS) void attn_combine_rows_kernel(AttnArgs a
         seg0 = b * a.direct;
     } else {
         const WorkList<kWorkUnit, false> list(a.seq_lens, a.B, a.max_seq_len, a.workers, own);
-        list.partials(b, seg0, n);
+        list.template partials<FIND == 3>(b, seg0, n);
     }
     const size_t base = ((size_t)h * a.rows_total + gr) * a.n_seg + seg0;
     const float4 *o4 = reinterpret_cast<const float4 *>(a.ws_o) + base * (kHeadDim / 4) + d4;
@@ -560,6 +561,8 @@ static void launch_combine_rows(int find, const AttnArgs &a, uint16_t *out, floa
     const dim3 grid((a.rows_total + ROWS - 1) / ROWS, a.geo.Hkv, a.B), block(32 * ROWS);
     if (find == 0)
         hipLaunchKernelGGL((attn_combine_rows_kernel<ROWS, 0>), grid, block, 0, stream, a, out, lse);
+    else if (find == 1 && a.even)
+        hipLaunchKernelGGL((attn_combine_rows_kernel<ROWS, 3>), grid, block, 0, stream, a, out, lse);
     else if (find == 1)
         hipLaunchKernelGGL((attn_combine_rows_kernel<ROWS, 1>), grid, block, 0, stream, a, out, lse);
     else
@@ -637,6 +640,15 @@ hipError_t launch_verify_tree(KvMode mode, const Geometry &g, const AttnPlan &pl
     return launch_tree_combine(a, each > 4 && fours <= resident_workgroups() ? 4 : 16, stream);
 }
 
+template <bool EVEN>
+static void launch_combine_deep(const AttnArgs &a, int max_live, uint16_t *out, float *lse, hipStream_t stream) {
+    const dim3 grid(a.rows_total, a.geo.Hkv, a.B);
+    if (max_live <= 64)
+        hipLaunchKernelGGL((attn_combine_kernel<8, EVEN>), grid, dim3(kCombineThreads), 0, stream, a, out, lse);
+    else
+        hipLaunchKernelGGL((attn_combine_kernel<16, EVEN>), grid, dim3(kCombineThreads), 0, stream, a, out, lse);
+}
+
 // The merge of the partials of `plan` and the tail.
 static hipError_t launch_combine(const AttnArgs &a, const AttnPlan &plan, uint16_t *out, float *lse, hipStream_t stream) {
     // Many partials a sequence: a row per workgroup, 8 threads deep in them, while
@@ -657,12 +669,10 @@ static hipError_t launch_combine(const AttnArgs &a, const AttnPlan &plan, uint16
             launch_combine_rows<4>(find, a, out, lse, stream);
         else
             launch_combine_rows<8>(find, a, out, lse, stream);
-    } else if (plan.max_live <= 64) {
-        hipLaunchKernelGGL(attn_combine_kernel<8>, dim3(plan.rows_total, a.geo.Hkv, a.B), dim3(kCombineThreads),
-                           0, stream, a, out, lse);
+    } else if (a.even) {
+        launch_combine_deep<true>(a, plan.max_live, out, lse, stream);
     } else {
-        hipLaunchKernelGGL(attn_combine_kernel<16>, dim3(plan.rows_total, a.geo.Hkv, a.B), dim3(kCombineThreads),
-                           0, stream, a, out, lse);
+        launch_combine_deep<false>(a, plan.max_live, out, lse, stream);
     }
     return hipGetLastError();
 }
@@ -802,6 +812,7 @@ hipError_t launch_attn_hier(const Geometry &g, const AttnPlan &plan, int B, int 
     a.max_live = plan.max_live;
     a.tail = n_tail > 0 ? 1 : 0;
     a.tail_first = n_tail - nq + 1;
+    a.even = true;
     a.tail_stride = n_tail;
     a.seq_lens = seq_lens;
     a.q = q;

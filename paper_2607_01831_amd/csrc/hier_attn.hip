@@ -31,16 +31,17 @@
 // some 250 vector instructions (450 from merged codes; a v_perm, a packed multiply-add or a conversion takes
 // 4.5 cycles of its SIMD) and 64 lookups (2.3 cycles of the CU's LDS each, 128 from
 // merged codes), then 35 instructions and 16 matrix products per 16 rows; 20 queries
-// over 32K of merged codes, 80 rows a kv head, 60.5 us.  Short ones, the launch and a
+// over 32K of merged codes, 80 rows a kv head, 55 us.  Short ones, the launch and a
 // chain of latencies: 4K 13.2 us.
 // Why so: the levels by table, since the transform's inverse is an exponential per
 // element; 64 copies of it, so that an address is one instruction (32 copies are read
 // as fast, but take two); lookups in batches of 16, what LDS counts; queries of 32 rows
-// at most, what two wavefronts a SIMD hold (64 and 80 rows at one a SIMD: 71 and 99 us
-// for the 60.5).  Operands made once for 64 to 256 rows by 8 wavefronts through LDS
+// at most, what two wavefronts a SIMD hold (with 64 and 80 rows at one a SIMD those 20
+// queries took 71 and 99 us, with 32 then 60.5).  Operands made once for 64 to 256 rows by 8 wavefronts through LDS
 // cost more up to 64 rows a kv head (38 us, so 40; 32K) and gain from 128 on (70 us,
 // so 59; 512 rows of 2 x 16K 157 us, so 120), with four times the partials that
-// lynx_attn_workspace_bytes has room for; with those that it has they lose.
+// lynx_attn_workspace_bytes has room for; with those that it has they lose.  Shares of
+// whole groups of 128 tokens: even_share.
 #include "f16_ops.h"
 #include "hier_ops.h"
 #include "lane_ops.h"
@@ -557,7 +558,7 @@ __global__ __launch_bounds__(kThreads, 2) void hier_attn_kernel(HierArgs a) {
         return;
     }
     const WorkList<kWorkUnit, true> list(a.seq_lens, a.B, a.max_seq_len, a.workers);
-    if (!seg.start(list, worker)) return;
+    if (!seg.start_even(list, worker)) return;
     fill_table<FULL>(a, lds);
     for (;;) {
         attend_segment<MT, FULL, LAYOUT, false>(a, seg, fresh_uniform(hc % a.geo.Hkv), fresh_uniform(hc / a.geo.Hkv),

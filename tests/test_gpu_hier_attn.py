@@ -125,6 +125,19 @@ def test_batches_of_many_units(B, most, bt, G, k, tail, full):
     Case(lens, 8, CENTRED if full else INT4, full, bt=bt, seed=B).check(8 * G, k, tail)
 
 
+RAGGED = (0, 1, 129, 4000, 7000, 513, 2900, 8000, 128, 64, 5000, 3100, 700, 2500, 4500, 1)
+
+
+@pytest.mark.parametrize("lens,G,k,tail,bt", [
+    (RAGGED, 4, 1, 0, 16), (RAGGED, 4, 1, 7, 16), (RAGGED[::-1], 2, 3, 4, 32), (RAGGED, 4, 5, 0, 48),
+    ((12000, 25000), 4, 2, 2, None), ((33000,), 4, 1, 0, None), ((33000,), 2, 2, 3, 16),
+    ((0, 36001), 4, 1, 0, 16), ((9000,) + tuple(range(400, 778, 6)), 2, 1, 1, 16),
+    ((512,) * 63 + (3000,), 2, 2, 2, 64), ((1100,) * 22 + (0,) * 42, 4, 1, 0, 16)])
+def test_shares_cut_inside_sequences(lens, G, k, tail, bt):
+    """More units than workers: shares of whole groups, of one sequence or of many."""
+    Case(lens, 8, INT4, bt=bt, seed=len(lens)).check(8 * G, k, tail)
+
+
 @pytest.mark.parametrize("variant,full", FORMS)
 @pytest.mark.parametrize("lens,Hkv,G,k,tail,bt", [((31, 0, 700), 2, 4, 3, 5, 16), ((130, 97), 2, 8, 9, 9, 48),
                                                   ((513,), 1, 5, 64, 64, 24), ((64, 1500), 1, 7, 20, 0, None)])
