@@ -23,6 +23,7 @@
 #include <stdint.h>
 
 #include <algorithm>
+#include <initializer_list>
 
 namespace {
 
@@ -202,6 +203,13 @@ int enter(PyObject *address, Call &c, Fn *, A... a) {
     return status;
 }
 long long positive(long long x) { return std::max(x, 0ll); }
+// A size in bytes that no tensor has where the product passes 64 bits.
+long long product(std::initializer_list<long long> factors) {
+    long long p = 1;
+    for (const long long f : factors)
+        if (__builtin_mul_overflow(p, f, &p)) return INT64_MAX;
+    return p;
+}
 
 constexpr auto kI32 = c10::kInt;
 constexpr auto kF32 = c10::kFloat;
@@ -213,10 +221,10 @@ PyObject *attn_hier(PyObject *, PyObject *const *a, Py_ssize_t n) {
         void *stream = c.pointer(a[2]);
         const Layout L = layout_of(c, a[3]);
         const int32_t B = c.i32(a[4]), Hq = c.i32(a[5]), k = c.i32(a[6]), most = c.i32(a[7]);
-        const long long nb = positive(B), heads = nb * L.kv_heads, io = nb * positive(k) * Hq;
+        const long long nb = positive(B), heads = nb * L.kv_heads, io = product({nb, positive(k), Hq, kHeadDim * 2});
         const int32_t full = c.truth(a[10]);
-        const long long plane = (long long)L.num_blocks * L.kv_heads * L.block_tokens * (full ? 128 : 64);
-        void *lens = c.tensor(a[8], nb * 4, kI32), *table = c.tensor(a[9], nb * L.max_blocks * 4, kI32);
+        const long long plane = product({L.num_blocks, L.kv_heads, L.block_tokens, full ? 128 : 64});
+        void *lens = c.tensor(a[8], nb * 4, kI32), *table = c.tensor(a[9], product({nb, L.max_blocks, 4}), kI32);
         void *kp = c.tensor(a[11], plane, kU8), *vp = c.tensor(a[12], plane, kU8);
         const float alpha = c.f32(a[13]);
         const int32_t variant = c.i32(a[14]);
@@ -224,10 +232,10 @@ PyObject *attn_hier(PyObject *, PyObject *const *a, Py_ssize_t n) {
         for (int i = 0; i < kMetaFields && c.ok; ++i) {
             PyObject *f = c.attribute(a[15], g_meta[i]);
             const int per = kMetaNames[i][2] == 'g' ? 256 : 32;
-            if (f) meta[i] = c.tensor(f, heads * ((L.max_tokens + (long long)per - 1) / per) * kHeadDim * 4, kF32);
+            if (f) meta[i] = c.tensor(f, product({heads, (L.max_tokens + (long long)per - 1) / per, kHeadDim * 4}), kF32);
             Py_XDECREF(f);
         }
-        void *q = c.tensor(a[16], io * kHeadDim * 2, kBF16);
+        void *q = c.tensor(a[16], io, kBF16);
         int32_t n_tail = 0;
         void *tail[2] = {nullptr, nullptr};
         if (a[17] == Py_None || a[18] == Py_None) {
@@ -237,10 +245,10 @@ PyObject *attn_hier(PyObject *, PyObject *const *a, Py_ssize_t n) {
                 c.ok = false;
             } else {
                 n_tail = (int32_t)t->size(1);
-                for (int i = 0; i < 2; ++i) tail[i] = c.tensor(a[17 + i], heads * n_tail * kHeadDim * 2, kBF16);
+                for (int i = 0; i < 2; ++i) tail[i] = c.tensor(a[17 + i], product({heads, n_tail, kHeadDim * 2}), kBF16);
             }
         }
-        void *out = c.tensor(a[19], io * kHeadDim * 2, kBF16), *lse = c.tensor(a[20], io * 4, kF32);
+        void *out = c.tensor(a[19], io, kBF16), *lse = c.tensor(a[20], product({nb, positive(k), Hq, 4}), kF32);
         if (PyLong_CheckExact(a[21])) c.ok = false;  // (its size is not known)
         void *ws = c.tensor(a[21], 0, kU8);
         if (!c.ok) return 0;
@@ -290,7 +298,7 @@ PyObject *qk_norm_rope(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const int32_t pairs = c.truth(a[12]);
         const float scale = c.f32(a[13]);
         void *out[3];
-        for (int i = 0; i < 3; ++i) out[i] = c.tensor(a[14 + i], i == 0 ? 0 : n_rows * H[1] * kHeadDim * 2, kBF16);
+        for (int i = 0; i < 3; ++i) out[i] = c.tensor(a[14 + i], i == 0 ? 0 : product({n_rows, H[1], kHeadDim * 2}), kBF16);
         if (!c.ok) return 0;
         using Fn = int(int32_t, int32_t, int32_t, int32_t, void *, int64_t, void *, int64_t, void *, int64_t, void *, void *,
                        int32_t, void *, void *, float, void *, int32_t, int32_t, float, void *, void *, void *, void *);
@@ -307,7 +315,7 @@ PyObject *blocks_extend(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const int32_t B = c.i32(a[4]), n_src = c.i32(a[5]);
         const long long nb = positive(B);
         void *lens = c.tensor(a[6], nb * 4, kI32), *counts = c.tensor(a[7], nb * 4, kI32);
-        void *table = c.tensor(a[8], nb * L.max_blocks * 4, kI32);
+        void *table = c.tensor(a[8], product({nb, L.max_blocks, 4}), kI32);
         void *stack = c.tensor(a[9], (long long)L.num_blocks * 4, kI32), *state = c.tensor(a[10], 8, kI32);
         void *granted = c.tensor(a[11], nb * 4, kI32), *starts = c.tensor(a[12], (nb + 1) * 4, kI32);
         long long rows = -1;
@@ -339,7 +347,7 @@ PyObject *blocks_release(PyObject *, PyObject *const *a, Py_ssize_t n) {
         const int32_t B = c.i32(a[4]);
         const long long nb = positive(B);
         void *lens = c.tensor(a[5], nb * 4, kI32), *keep = c.tensor(a[6], nb * 4, kI32);
-        void *table = c.tensor(a[7], nb * L.max_blocks * 4, kI32);
+        void *table = c.tensor(a[7], product({nb, L.max_blocks, 4}), kI32);
         void *stack = c.tensor(a[8], (long long)L.num_blocks * 4, kI32), *state = c.tensor(a[9], 8, kI32);
         if (!c.ok) return 0;
         using Fn = int(const Layout *, int32_t, void *, void *, void *, void *, void *, void *);

@@ -64,7 +64,7 @@ def test_qk_norm_rope_refusals(lib):
                 dict(eps=-1e-6), dict(eps=math.nan), dict(eps=math.inf), dict(freq=None), dict(freq=8), dict(rotary=-16),
                 dict(rotary=144), dict(rotary=24), dict(rotary=8), dict(pairs=2), dict(pairs=-1), dict(scale=math.nan),
                 dict(scale=math.inf), dict(qo=None), dict(qo=8), dict(ko=None), dict(ko=8), dict(qo=1 << 20),
-                dict(ko=(1 << 20) + 3 * 3072 + 512 * 2 - 16), dict(vo=(1 << 20) - 4 * 256 * 2 + 16), dict(qo=(1 << 20) - 16),
+                dict(ko=(1 << 20) + 3 * 1536 * 2 + 512 * 2 - 16), dict(vo=(1 << 20) - 4 * 256 * 2 + 16), dict(qo=(1 << 20) - 16),
                 dict(ko=2 << 20), dict(vo=3 << 20), dict(vo=(2 << 20) + 4 * 8 * 256 - 16)):
         assert call(**bad) == E.LYNX_EINVAL, bad
     none = dict(q=None, k=None, v=None, pos=None, qw=None, kw=None, freq=None, qo=None, ko=None, vo=None)
