@@ -187,8 +187,9 @@ __global__ __launch_bounds__(THREADS) void blocks_release_kernel(BlocksArgs a, i
     for (int b = b0; b < b1; ++b) drop += drop_of(b, keep);
     s_first[tid] = scan_before<THREADS>(drop, s_wave, total);
     __syncthreads();
-    for (int n = blockIdx.x * THREADS + tid; n < total; n += gridDim.x * THREADS) {
-        const int t = find_last<THREADS>(s_first, n);
+    // (64 bits: the last step goes past the total, which may be 2^31 - 1)
+    for (int64_t at = blockIdx.x * THREADS + tid; at < total; at += gridDim.x * THREADS) {
+        const int n = (int)at, t = find_last<THREADS>(s_first, n);
         int f = s_first[t], b, d;
         for (b = t * per;; ++b) {  // ends: block n is one of theirs
             d = drop_of(b, keep);
@@ -196,8 +197,8 @@ __global__ __launch_bounds__(THREADS) void blocks_release_kernel(BlocksArgs a, i
             f += d;
         }
         int32_t *entry = a.block_table + (size_t)b * a.max_blocks + keep + (n - f);
-        const int64_t at = (int64_t)free + total - 1 - n;
-        if (at < a.num_blocks) a.free_blocks[at] = *entry;
+        const int64_t top = (int64_t)free + total - 1 - n;
+        if (top < a.num_blocks) a.free_blocks[top] = *entry;
         *entry = -1;
     }
     settle<THREADS>(a.state, (int)min((int64_t)free + total, (int64_t)a.num_blocks), &s_flag);
