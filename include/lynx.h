@@ -834,7 +834,9 @@ int lynx_blocks_extend(const lynx_layout *L, int32_t B, int32_t n_src, int32_t m
  *   block_table  the entries of those blocks become -1
  *   free_blocks, free_state   the ids are pushed so that the first sequence's first
  *                block is on top: releasing what an extend took restores the stack.
- *                Ids that num_blocks leaves no room for are dropped
+ *                Entries outside [0, num_blocks) (a sequence released twice) are not
+ *                pushed; ids that num_blocks leaves no room for are dropped, those
+ *                of the first sequences
  * Launches one kernel.
  */
 int lynx_blocks_release(const lynx_layout *L, int32_t B, const int32_t *seq_lens,

@@ -169,11 +169,33 @@ __global__ __launch_bounds__(THREADS) void blocks_extend_kernel(BlocksArgs a, in
     settle<THREADS>(a.state, free - total_taken, &s_flag);
 }
 
+// Of n ids, the lowest on the stack first, those of the pool go on it from `at` up, in
+// their order, while there is room: how many.  id_of(i) may read what lies at `at` + i.
+template <int THREADS, typename Id>
+__device__ int push_valid(const BlocksArgs &a, int at, int n, int *s_wave, Id id_of) {
+    int64_t count = 0;
+    for (int64_t i0 = 0; i0 < n; i0 += THREADS) {
+        const int64_t i = i0 + threadIdx.x;
+        const int id = i < n ? id_of((int)i) : -1;
+        const bool valid = id >= 0 && id < a.num_blocks;
+        int all;
+        const int64_t to = at + count + scan_before<THREADS>(valid, s_wave, all);
+        if (valid && to < a.num_blocks) a.free_blocks[to] = id;
+        count = min(count + all, (int64_t)a.num_blocks - at);
+    }
+    return (int)count;
+}
+
 // seq_lens: tokens held; counts: tokens kept.  The blocks behind those go back, the
-// first one of the first sequence on top.
+// first one of the first sequence on top.  An entry that holds no block (of a sequence
+// given back before) is left out, which only a count of the valid ones before it can
+// do; so all are stored as if they were valid, and the last workgroup to arrive closes
+// the gaps where any of them saw an invalid one.  Where that many would not fit the
+// stack, as happens with invalid ones alone, it pushes the valid ones by itself.
 template <int THREADS>
 __global__ __launch_bounds__(THREADS) void blocks_release_kernel(BlocksArgs a, int per) {
-    __shared__ int s_wave[THREADS / 64], s_flag;
+    __shared__ int s_wave[THREADS / 64];
+    __shared__ unsigned s_seen;
     __shared__ int s_first[THREADS];
     const int tid = threadIdx.x;
     const int b0 = tid * per, b1 = min(b0 + per, a.B);
@@ -187,9 +209,9 @@ __global__ __launch_bounds__(THREADS) void blocks_release_kernel(BlocksArgs a, i
     for (int b = b0; b < b1; ++b) drop += drop_of(b, keep);
     s_first[tid] = scan_before<THREADS>(drop, s_wave, total);
     __syncthreads();
-    // (64 bits: the last step goes past the total, which may be 2^31 - 1)
-    for (int64_t at = blockIdx.x * THREADS + tid; at < total; at += gridDim.x * THREADS) {
-        const int n = (int)at, t = find_last<THREADS>(s_first, n);
+    // Block n of them: its id, the table's entry cleared.
+    auto take = [&](int n) {
+        const int t = find_last<THREADS>(s_first, n);
         int f = s_first[t], b, d;
         for (b = t * per;; ++b) {  // ends: block n is one of theirs
             d = drop_of(b, keep);
@@ -197,11 +219,39 @@ __global__ __launch_bounds__(THREADS) void blocks_release_kernel(BlocksArgs a, i
             f += d;
         }
         int32_t *entry = a.block_table + (size_t)b * a.max_blocks + keep + (n - f);
-        const int64_t top = (int64_t)free + total - 1 - n;
-        if (top < a.num_blocks) a.free_blocks[top] = *entry;
+        const int id = *entry;
         *entry = -1;
+        return id;
+    };
+    const bool room = (int64_t)free + total <= a.num_blocks;
+    bool invalid = false;
+    if (room)
+        // (64 bits: the last step goes past the total, which may be 2^31 - 1)
+        for (int64_t n = blockIdx.x * THREADS + tid; n < total; n += gridDim.x * THREADS) {
+            const int id = take((int)n);
+            invalid |= id < 0 || id >= a.num_blocks;
+            // (through to memory: another workgroup may close the gaps)
+            __hip_atomic_store(a.free_blocks + (free + total - 1 - n), id, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        }
+    // ---- arrivals in the low 16 bits of the second word, above them who saw one ----
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+    unsigned gaps = __syncthreads_or(invalid) ? 1u << 16 : 0u;
+    if (gridDim.x > 1) {
+        unsigned *word = reinterpret_cast<unsigned *>(a.state + 1);
+        if (tid == 0) s_seen = gaps + __hip_atomic_fetch_add(word, 1u + gaps, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        __syncthreads();
+        if ((s_seen & 0xffffu) != gridDim.x - 1) return;
+        gaps = s_seen >> 16;
+        if (tid == 0) __hip_atomic_store(word, 0u, __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
     }
-    settle<THREADS>(a.state, (int)min((int64_t)free + total, (int64_t)a.num_blocks), &s_flag);
+    int pushed = total;
+    if (!room)
+        pushed = push_valid<THREADS>(a, free, total, s_wave, [&](int i) { return take(total - 1 - i); });
+    else if (gaps)
+        pushed = push_valid<THREADS>(a, free, total, s_wave, [&](int i) {
+            return __hip_atomic_load(a.free_blocks + (free + i), __ATOMIC_RELAXED, __HIP_MEMORY_SCOPE_AGENT);
+        });
+    if (tid == 0) a.state[0] = free + pushed;
 }
 
 }  // namespace

@@ -26,3 +26,98 @@ def test_release_of_nearly_2_31_blocks():
     # the first sequence's first block on top
     assert torch.equal(stack[:total], torch.arange(total - 1, -1, -1, dtype=torch.int32, device="cuda"))
     assert (stack[total:] == -9).all()
+
+
+def released(lens, keep, table, stack, n_free, bt, n_blocks):
+    """The release in Python, only ids of the pool given back: the number on the stack;
+    the lists change in place."""
+    back = []
+    for b, (n, k) in enumerate(zip(lens, keep)):
+        for j in range(-(-min(k, n) // bt), -(-n // bt)):
+            back.append(table[b][j])
+            table[b][j] = -1
+    for x in reversed(back):
+        if 0 <= x < n_blocks and n_free < n_blocks:
+            stack[n_free] = x
+            n_free += 1
+    return n_free
+
+
+class Blocks:
+    """Sequences of `lens` tokens with a pool of `spare` blocks more than they hold."""
+
+    def __init__(self, lens, bt, per, spare, seed=0):
+        self.lens, self.bt, held = list(lens), bt, [-(-n // bt) for n in lens]
+        self.n_blocks = sum(held) + spare
+        ids = torch.randperm(self.n_blocks, generator=torch.Generator().manual_seed(seed)).tolist()
+        self.table = [[ids.pop() for _ in range(h)] + [-1] * (per - h) for h in held]
+        self.stack, self.free = ids + [-9] * (self.n_blocks - len(ids)), len(ids)
+        self.L = lynx.Layout(num_kv_heads=1, block_tokens=bt, max_blocks_per_seq=per, num_blocks=self.n_blocks,
+                             max_tokens=per * bt)
+        self.upload()
+
+    def upload(self):
+        ints = lambda x: torch.tensor(x, dtype=torch.int32).cuda()  # noqa: E731
+        self.dev = [ints(self.table), ints(self.stack), ints([self.free, 0])]
+
+    def release(self, keep, lens=None):
+        lens = self.lens if lens is None else lens
+        note(f"blocks_release B={len(lens)} bt={self.bt} free={self.free} of {self.n_blocks}")
+        d_lens, d_keep = (torch.tensor(x, dtype=torch.int32).cuda() for x in (lens, keep))
+        lynx.lynx_blocks_release(self.L, len(lens), d_lens, d_keep, *self.dev)
+        self.free = released(lens, keep, self.table, self.stack, self.free, self.bt, self.n_blocks)
+        table, stack, state = (x.tolist() for x in self.dev)
+        assert state == [self.free, 0] and table == self.table
+        assert stack[:self.free] == self.stack[:self.free]  # (above the count the stack holds nothing)
+        self.stack = stack
+
+
+# one workgroup, several of 256 threads, several of 1024
+@pytest.mark.parametrize("B,per", [(2, 8), (5, 40), (64, 200), (256, 80), (300, 300), (1500, 40)])
+def test_sequences_released_twice(B, per):
+    """Nothing is pushed twice, and the blocks of the others are not lost, whether
+    there would have been room for what is pushed in vain or not."""
+    g = torch.Generator().manual_seed(B)
+    lens = torch.randint(1, 4 * per + 1, (B,), generator=g).tolist()
+    p = Blocks(lens, 4, per, spare=3, seed=B)
+    some = [0 if b % 3 == 0 else n for b, n in enumerate(lens)]
+    p.release(some)                            # a third of them done
+    p.release([n // 2 for n in lens])          # ... and once more, beside half of the others
+    p.release([0] * B)
+    assert p.free == p.n_blocks and sorted(p.stack) == list(range(p.n_blocks))
+    p.release([0] * B)                         # all of them a second time
+    assert p.free == p.n_blocks and sorted(p.stack) == list(range(p.n_blocks))
+
+
+@pytest.mark.parametrize("free", [0, 7, 10 ** 6])
+@pytest.mark.parametrize("B,per", [(3, 30), (60, 300), (400, 120)])
+def test_entries_outside_the_pool(B, per, free):
+    """Among the blocks given back; `free` ids on the stack, or as many as leave no
+    room for the last."""
+    g = torch.Generator().manual_seed(B + free)
+    p = Blocks(torch.randint(0, 4 * per + 1, (B,), generator=g).tolist(), 4, per, spare=0, seed=B)
+    held = p.n_blocks
+    for bad in (-1, p.n_blocks, 2 ** 31 - 1, -2 ** 31):
+        for _ in range(max(1, held // 40)):
+            b = int(torch.randint(0, B, (1,), generator=g))
+            p.table[b][int(torch.randint(0, per, (1,), generator=g))] = bad
+    p.free = max(0, min(free, held - 5))
+    p.stack[:p.free] = range(p.free)
+    p.upload()
+    p.release([n // 3 for n in p.lens])
+
+
+def test_captured_releases():
+    """Replays after the first give the same sequences back again."""
+    p = Blocks([40, 9, 77] * 30, 2, 39, spare=0)
+    keep = [0, 9, 50] * 30
+    d_lens, d_keep = (torch.tensor(x, dtype=torch.int32).cuda() for x in (p.lens, keep))
+    torch.cuda.synchronize()
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        lynx.lynx_blocks_release(p.L, len(keep), d_lens, d_keep, *p.dev)
+    for _ in range(3):
+        graph.replay()
+        p.free = released(p.lens, keep, p.table, p.stack, p.free, p.bt, p.n_blocks)
+        table, stack, state = (x.tolist() for x in p.dev)
+        assert state == [p.free, 0] and table == p.table and stack[:p.free] == p.stack[:p.free]
