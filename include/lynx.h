@@ -770,8 +770,9 @@ int lynx_attn_hier(const lynx_layout *L, int32_t B, int32_t Hq, int32_t k, int32
  *   scale        of the rotated dims (1, or a long-context factor)
  *   q_out        BF16 [n_rows][Hq][128]; k_out, v_out BF16 [n_rows][Hkv][128]
  *                (device, written; rows of no token are left as they were).
- *                None may overlap an input or another (LYNX_EINVAL: the bytes
- *                between an input's first token and the end of its last count)
+ *                None may overlap another or any array that is read (LYNX_EINVAL:
+ *                of q, k and v the bytes between the first token and the end of
+ *                the last count)
  */
 int lynx_qk_norm_rope(int32_t n_tokens, int32_t Hq, int32_t Hkv, int32_t head_dim,
                       const void *q_bf16, int64_t q_stride, const void *k_bf16, int64_t k_stride,

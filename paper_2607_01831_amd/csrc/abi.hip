@@ -825,17 +825,20 @@ int lynx_qk_norm_rope(int32_t n_tokens, int32_t Hq, int32_t Hkv, int32_t head_di
         if (!aligned16(p)) return LYNX_EINVAL;
     if (rotary_dim > 0 && !inv_freq) return LYNX_EINVAL;
     // no output may overlap an input or another output
-    const struct { const void *p; int64_t rows, stride, heads; } in[] = {
-        {q_bf16, n_tokens, q_stride, Hq}, {k_bf16, n_tokens, k_stride, Hkv}, {v_bf16, n_tokens, v_stride, Hkv},
-        {q_out, n_rows, (int64_t)Hq * lynx::kHeadDim, Hq}, {k_out, n_rows, (int64_t)Hkv * lynx::kHeadDim, Hkv}};
-    const struct { const void *p; int64_t heads; } out[] = {{q_out, Hq}, {k_out, Hkv}, {v_out, Hkv}};
-    for (const auto &i : in)
-        for (const auto &o : out) {
-            if (!i.p || !o.p || &i - in == &o - out + 3) continue;
-            const uintptr_t i0 = reinterpret_cast<uintptr_t>(i.p), o0 = reinterpret_cast<uintptr_t>(o.p);
-            const uintptr_t i1 = i0 + ((i.rows - 1) * i.stride + i.heads * lynx::kHeadDim) * 2;
-            const uintptr_t o1 = o0 + (uintptr_t)n_rows * o.heads * lynx::kHeadDim * 2;
-            if (i0 < o1 && o0 < i1) return LYNX_EINVAL;
+    auto tokens = [&](int64_t stride, int64_t heads) {
+        return (uint64_t)((n_tokens - 1) * stride + heads * lynx::kHeadDim) * 2;
+    };
+    auto rows_of = [&](int64_t heads) { return (uint64_t)n_rows * heads * lynx::kHeadDim * 2; };
+    const struct { const void *p; uint64_t bytes; } arrays[] = {
+        {q_out, rows_of(Hq)}, {k_out, rows_of(Hkv)}, {v_out, rows_of(Hkv)},
+        {q_bf16, tokens(q_stride, Hq)}, {k_bf16, tokens(k_stride, Hkv)}, {v_bf16, tokens(v_stride, Hkv)},
+        {positions, 4ull * n_tokens}, {rows, 4ull * n_tokens}, {q_weight, 2 * lynx::kHeadDim},
+        {k_weight, 2 * lynx::kHeadDim}, {inv_freq, 2ull * rotary_dim}};
+    for (int o = 0; o < 3; ++o)
+        for (size_t i = o + 1; i < sizeof(arrays) / sizeof(arrays[0]); ++i) {
+            if (!arrays[i].p || !arrays[o].p) continue;
+            const uintptr_t i0 = reinterpret_cast<uintptr_t>(arrays[i].p), o0 = reinterpret_cast<uintptr_t>(arrays[o].p);
+            if (i0 < o0 + arrays[o].bytes && o0 < i0 + arrays[i].bytes) return LYNX_EINVAL;
         }
     lynx::RopeArgs a;
     a.n_tokens = n_tokens;
