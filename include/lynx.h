@@ -818,8 +818,10 @@ int lynx_qk_norm_rope(int32_t n_tokens, int32_t Hq, int32_t Hkv, int32_t head_di
  *                outside [0, num_blocks); and its row b * n_src + i in arrays
  *                [B][n_src] (new token i of the sequence), as `rows` of
  *                lynx_qk_norm_rope fills them.  -1 from starts[B] on
- * No written array may overlap another (LYNX_EINVAL); num_blocks * block_tokens and
- * B * max_blocks_per_seq must be less than 2^31.  B <= 65535.  Launches one kernel.
+ * B == 0: starts[0] is 0 and the token arrays are -1 (free_state NULL: nothing is
+ * written).  No written array may overlap another (LYNX_EINVAL);
+ * num_blocks * block_tokens and B * max_blocks_per_seq must be less than 2^31.
+ * B <= 65535.  Launches one kernel.
  */
 int lynx_blocks_extend(const lynx_layout *L, int32_t B, int32_t n_src, int32_t max_rows,
                        const int32_t *seq_lens, const int32_t *counts, int32_t *block_table,

@@ -923,10 +923,9 @@ int lynx_blocks_extend(const lynx_layout *L, int32_t B, int32_t n_src, int32_t m
     int rc = blocks_args(L, B, seq_lens, counts, block_table, const_cast<int32_t *>(free_blocks), free_state, &a);
     if (rc != LYNX_OK) return rc;
     if (n_src < 0 || (long long)B * n_src > INT32_MAX || max_rows < 0 || max_rows > (1 << 30)) return LYNX_EINVAL;
-    if (B == 0) return LYNX_OK;
-    const void *ptrs[] = {granted, starts};
-    for (const void *p : ptrs)
-        if (!p || !aligned16(p)) return LYNX_EINVAL;
+    if (B == 0 && !free_state) return LYNX_OK;  // (else the plan of no sequence is written)
+    if (!aligned16(free_state)) return LYNX_EINVAL;
+    if ((B > 0 && !granted) || !aligned16(granted) || !starts || !aligned16(starts)) return LYNX_EINVAL;
     const void *may_be_null[] = {seq_of, positions, slots, rows};
     for (const void *p : may_be_null)
         if (!aligned16(p)) return LYNX_EINVAL;

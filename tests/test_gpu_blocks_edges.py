@@ -121,3 +121,21 @@ def test_captured_releases():
         p.free = released(p.lens, keep, p.table, p.stack, p.free, p.bt, p.n_blocks)
         table, stack, state = (x.tolist() for x in p.dev)
         assert state == [p.free, 0] and table == p.table and stack[:p.free] == p.stack[:p.free]
+
+
+@pytest.mark.parametrize("whole", [True, False])
+@pytest.mark.parametrize("rows", [0, 1, 5000])
+def test_a_step_of_no_sequences(rows, whole, monkeypatch):
+    """Its plan is written like any other: no token stands in it."""
+    if not whole:
+        monkeypatch.setattr(lynx, "_whole", lambda *args: None)
+    L = lynx.Layout(num_kv_heads=1, block_tokens=16, max_blocks_per_seq=4, num_blocks=9, max_tokens=64)
+    free = lynx.FreeBlocks.allocate(L, 0)
+    ints = lambda n: torch.full((n,), 77, dtype=torch.int32, device="cuda")  # noqa: E731
+    none, starts, outs = ints(0), ints(1), [ints(rows) for _ in range(4)]
+    note(f"blocks_extend B=0 rows={rows}")
+    lynx.lynx_blocks_extend(L, 0, 3, none, none, free.table, free.stack, free.state, none, starts, *outs)
+    assert starts.tolist() == [0] and free.state.tolist() == [9, 0] and free.stack.tolist() == list(range(8, -1, -1))
+    assert all((x == -1).all() for x in outs)
+    lynx.lynx_blocks_release(L, 0, none, none, free.table, free.stack, free.state)
+    assert free.state.tolist() == [9, 0]
