@@ -731,9 +731,11 @@ int lynx_kv_dequant(const lynx_layout *L, int32_t B, int32_t max_n, const int32_
  * A query that sees no token yields zeros and lse = -inf; the rows of a sequence
  * one of whose block ids is outside [0, num_blocks) are NaN.
  * Precision: with b = sigma * gscale and m = mu * gscale + gmin, a key or value
- * x = +-level b + m of the context is off by at most 2^-11 (2 |level b| + |m| + |x|)
- * (2^-37 of the largest of the context), a weight by 2^-11 of itself (2^-32 of the
- * row's largest).
+ * x = +-level b + m of the context is off by at most 2^-11 (2 |level b| + |m| + |x|),
+ * and 2^-25 |b| (levels below 2^-14, as alpha of 1000 and more gives them to the
+ * smallest codes), and 2^-36 of the largest |b| + |m| of the context; a weight by
+ * 2^-11 of itself, and 2^-32 of the row's largest; a query's element by 2^-34 of its
+ * row's largest where it is below 2^-26 of that.
  */
 int lynx_attn_hier(const lynx_layout *L, int32_t B, int32_t Hq, int32_t k, int32_t max_seq_len,
                    const int32_t *seq_lens, const int32_t *block_table, int32_t full,

@@ -19,11 +19,14 @@
 // Rounding.  A level, b, m and x are rounded to fp16 (11 significant bits, 2^-11 of
 // themselves at most), so x is off by at most 2^-11 (2 |level b| + |m| + |x|), an
 // eighth of what so many roundings to BF16 would be; a softmax weight is rounded
-// likewise (2^-11 of itself, 2^-32 of the row's largest).  Queries are BF16 and
-// exact.  Scores, softmax statistics and outputs are fp32.  Powers of two keep the
+// likewise (2^-11 of itself, 2^-32 of the row's largest).  Scores, softmax statistics
+// and outputs are fp32.  Powers of two keep the
 // operands in fp16's range whatever the cache's: K and V are scaled by an exponent
 // each that brings the largest |b| + |m| so far below 2^14, so values 2^-28 of the
-// largest lose bits; a query row by its largest element.
+// largest lose bits: b, m and x 2^-25 each, three times 2^-38 of the largest; a query
+// row by its largest element to below 2^10, so its elements from 2^-26 of that on are
+// exact and smaller ones off by 2^-34 of it.  A level is not scaled: below 2^-14, where
+// alpha of 1000 and more puts the smallest codes, it is off by 2^-25, x by that of b.
 //
 // What bounds it.  Long decodes, memory: 4 sequences of 64K, 64 heads over 8, 84.5 us,
 // 419 MB, 5.0 TB/s (a large copy 5.1); with its loads left out the same takes 58 us.
