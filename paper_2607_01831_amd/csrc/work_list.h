@@ -142,11 +142,12 @@ struct WorkList {
     // (start_even): the smallest share, a unit at least and at most three groups more
     // than the equal ones' largest, that takes no more workers.  The hierarchical
     // attention against the shares of inner_share, 16 paged sequences of 1K-8K: 38.3
-    // us, so 41.4; 20 rows each 57.5, so 64.2; one of 32K, 80 rows 56.3, so 61.8; 3 of
-    // 1K-9K, 256 rows 77, so 84; where both end at the same share (32 of up to 4K) 53.3
-    // and 52.8.
+    // us, so 41.4; 20 rows each 57.5, so 64.2; 3 of 1K-9K, 256 rows 77, so 84; where
+    // both end at the same share (32 of up to 4K) 53.3 and 52.8.  Fewer workers than
+    // sequences have no such share, which every workgroup would find out in up to 200
+    // steps (64 sequences of 200 tokens, 512 rows a kv head: 703 us, without them 467).
     __device__ __forceinline__ int even_share(int &segs) const {
-        if (B == 1 || B > 64 || workers == total) return 0;
+        if (B == 1 || B > 64 || workers < B || workers == total) return 0;
         const uint32_t groups = (int)(threadIdx.x & 63) < B ? max(1u, ((uint32_t)own_T + kKGroup - 1) / kKGroup) : 0u;
         const uint32_t all = (uint32_t)__builtin_amdgcn_readlane(scan((int)groups), 63), w = (uint32_t)opaque(workers);
         const uint32_t most = UNIT * (((uint32_t)total + w - 1) / w) + UNIT - 1;
@@ -237,7 +238,8 @@ struct Segment {
         return true;
     }
     // The same, the shares cut in groups: those of a single sequence, and those inside
-    // sequences (even_share), each sequence's as equal as its groups allow.
+    // sequences (even_share), each sequence's as equal as its groups allow.  One of 32K,
+    // 80 rows a kv head, against shares of whole units: 56.3 us, so 61.8.
     template <bool WALK>
     __device__ __forceinline__ bool start_even(const WorkList<UNIT, WALK> &wl, int p) {
         if (p >= wl.workers) return false;
