@@ -752,7 +752,8 @@ int lynx_attn_hier(const lynx_layout *L, int32_t B, int32_t Hq, int32_t k, int32
  *   y = x * rsqrt(mean(x^2) + eps) * weight, or x where the weights are NULL;
  *   of the first rotary_dim dims, pairs (a, b) become
  *   (a cos - b sin, b cos + a sin) * scale with the angle position * inv_freq[i],
- *   taken exactly however far the position is.
+ *   reduced in double precision (off by 1e-7 of a turn at most, however far the
+ *   position, for frequencies up to 1).
  * V is moved as it is.
  *
  *   head_dim     must be 128 (LYNX_ENOTSUP)

@@ -15,8 +15,9 @@
 // An entry of the table that this call writes is read from the stack by whoever
 // needs it, an entry read from the table is never one that this call writes.  Only
 // the stack's counter needs all to have read it before it moves: the last workgroup
-// to arrive writes it.  Either call takes 4.5 us with the host's part, from one
-// sequence to 500 with 131072 rows.
+// to arrive writes it.  The kernels take 3.0 and 1.9 us for one sequence, 3.8 and 3.6
+// for 64 with 8 tokens each, 7.3 and 5.6 for 500 with 131072 rows (a call of the host
+// 4.5).
 #include "lane_ops.h"
 #include "lynx_internal.h"
 #include "split_merge.h"

@@ -20,31 +20,32 @@
 // themselves at most), so x is off by at most 2^-11 (2 |level b| + |m| + |x|), an
 // eighth of what so many roundings to BF16 would be; a softmax weight is rounded
 // likewise (2^-11 of itself, 2^-32 of the row's largest).  Scores, softmax statistics
-// and outputs are fp32.  Powers of two keep the
-// operands in fp16's range whatever the cache's: K and V are scaled by an exponent
-// each that brings the largest |b| + |m| so far below 2^14, so values 2^-28 of the
-// largest lose bits: b, m and x 2^-25 each, three times 2^-38 of the largest; a query
-// row by its largest element to below 2^10, so its elements from 2^-26 of that on are
-// exact and smaller ones off by 2^-34 of it.  A level is not scaled: below 2^-14, where
-// alpha of 1000 and more puts the smallest codes, it is off by 2^-25, x by that of b.
+// and outputs are fp32.  Powers of two keep the operands in fp16's range whatever the
+// cache's: K and V are scaled by an exponent each that brings the largest |b| + |m| so
+// far below 2^14, so values 2^-28 of the largest lose bits: b, m and x 2^-25 each, three
+// times 2^-38 of the largest; a query row by its largest element to below 2^10, so its
+// elements from 2^-26 of that on are exact and smaller ones off by 2^-34 of it.  A level
+// is not scaled: below 2^-14, where alpha of 1000 and more puts the smallest codes, it
+// is off by 2^-25, x by that of b.
 //
-// What bounds it.  Long decodes, memory: 4 sequences of 64K, 64 heads over 8, 84.5 us,
-// 419 MB, 5.0 TB/s (a large copy 5.1); with its loads left out the same takes 58 us.
+// What bounds it.  Long decodes, memory: 4 sequences of 64K, 64 heads over 8, 85.6 us,
+// 419 MB, 4.9 TB/s (a large copy 5.1); with its loads left out the same takes 58 us.
 // Many rows, the vector ALU and LDS: per 32 tokens a wavefront makes operands in
-// some 250 vector instructions (450 from merged codes; a v_perm, a packed multiply-add or a conversion takes
-// 4.5 cycles of its SIMD) and 64 lookups (2.3 cycles of the CU's LDS each, 128 from
-// merged codes), then 35 instructions and 16 matrix products per 16 rows; 20 queries
-// over 32K of merged codes, 80 rows a kv head, 55 us.  Short ones, the launch and a
-// chain of latencies: 4K 13.2 us.
+// some 250 vector instructions (450 from merged codes; a v_perm, a packed multiply-add
+// or a conversion takes 4.5 cycles of its SIMD) and 64 lookups (2.3 cycles of the CU's
+// LDS each, 128 from merged codes), then 35 instructions and 16 matrix products per 16
+// rows; 20 queries over 32K of merged codes, 80 rows a kv head, 54 us.  Short ones, the
+// launch and a chain of latencies: 4K 13.1 us.
 // Why so: the levels by table, since the transform's inverse is an exponential per
 // element; 64 copies of it, so that an address is one instruction (32 copies are read
 // as fast, but take two); lookups in batches of 16, what LDS counts; queries of 32 rows
-// at most, what two wavefronts a SIMD hold (with 64 and 80 rows at one a SIMD those 20
-// queries took 71 and 99 us, with 32 then 60.5).  Operands made once for 64 to 256 rows by 8 wavefronts through LDS
-// cost more up to 64 rows a kv head (38 us, so 40; 32K) and gain from 128 on (70 us,
-// so 59; 512 rows of 2 x 16K 157 us, so 120), with four times the partials that
-// lynx_attn_workspace_bytes has room for; with those that it has they lose.  Shares of
-// whole groups of 128 tokens: even_share.
+// at most, what two wavefronts a SIMD hold (before shares were cut in groups those 20
+// queries took 60.5 us, with 64 and 80 rows at one a SIMD 71 and 99).  Operands made
+// once for 64 to 256 rows by 8 wavefronts through LDS cost more up to 64 rows a kv head
+// (38 us, so 40; 32K) and gain from 128 on (70 us, so 59; 512 rows of 2 x 16K 157 us, so
+// 120) where the workspace holds four times the partials; it is not built, since this
+// call takes the workspace of the other attention calls, with which it loses (256 rows
+// of 32K 90 us, so 151).  Shares of whole groups of 128 tokens: even_share.
 #include "f16_ops.h"
 #include "hier_ops.h"
 #include "lane_ops.h"
@@ -592,9 +593,9 @@ void launch_layout(const HierArgs &args, dim3 grid, hipStream_t stream) {
 }  // namespace
 
 // 32 rows a workgroup where there are more than 16, whose operands are then made half
-// as often: 20 rows of 32K 26.7 us, so 29.9 in tiles of 16; 80 rows 61.5, so 71.2;
-// 16 paged sequences of 1K-8K with 20 rows 55, so 70 (32 rows of 2000 tokens, all
-// latency, 20.3, so 17.4).
+// as often: 20 rows of 32K of merged codes 29.8 us, so 37.2 in tiles of 16; 80 rows
+// 55.6, so 67.7; 16 paged sequences of 1K-8K with 20 rows 56.5, so 75.6 (32 rows of 2000
+// tokens, all latency, 20.6, so 17.5).
 hipError_t launch_hier_attn(const HierArgs &args, hipStream_t stream) {
     if (args.workers < 1 || args.workers > 65535) return hipErrorInvalidValue;
     const int tile = args.rows_total > 16 ? 32 : 16;

@@ -32,9 +32,8 @@ __device__ __forceinline__ SignedCode signed_code(int variant, uint32_t qa, uint
 
 // The signed level as fp16: expm1(code / M log1p(alpha)) / alpha, 0 .. 1, rounded to
 // nearest (2^-11 of itself, or by 2^-25 below 2^-14: the smallest codes of an alpha of
-// 1000 and more).  log1p_alpha is rounded
-// from double on the host; a tiny alpha takes the first two terms of the series,
-// where expm1's argument would be a denormal.
+// 1000 and more).  log1p_alpha is rounded from double on the host; a tiny alpha takes
+// the first two terms of the series, where expm1's argument would be a denormal.
 template <int FULL>
 __device__ __forceinline__ _Float16 signed_level_f16(float alpha, float log1p_alpha, int variant, uint32_t qa,
                                                      uint32_t qr) {
