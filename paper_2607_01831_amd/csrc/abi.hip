@@ -831,7 +831,7 @@ int lynx_qk_norm_rope(int32_t n_tokens, int32_t Hq, int32_t Hkv, int32_t head_di
     auto rows_of = [&](int64_t heads) { return (uint64_t)n_rows * heads * lynx::kHeadDim * 2; };
     const struct { const void *p; uint64_t bytes; } arrays[] = {
         {q_out, rows_of(Hq)}, {k_out, rows_of(Hkv)}, {v_out, rows_of(Hkv)},
-        {q_bf16, tokens(q_stride, Hq)}, {k_bf16, tokens(k_stride, Hkv)}, {v_bf16, tokens(v_stride, Hkv)},
+        {q_bf16, tokens(strides[0], Hq)}, {k_bf16, tokens(strides[1], Hkv)}, {v_bf16, tokens(strides[2], Hkv)},
         {positions, 4ull * n_tokens}, {rows, 4ull * n_tokens}, {q_weight, 2 * lynx::kHeadDim},
         {k_weight, 2 * lynx::kHeadDim}, {inv_freq, 2ull * rotary_dim}};
     for (int o = 0; o < 3; ++o)
